@@ -320,6 +320,114 @@ int ptq4vm_f16_linear(const void *x_f16, const void *w_f16, const void *bias_f16
                       int64_t M, int64_t K, int64_t N, int64_t ldx, int64_t ldw, int64_t ldy,
                       void *stream);
 
+/*
+ * The operators between a block's linears.  Beside fp16 they take bfloat16 and fp32: `dtype` is the type T of the matrices
+ * (activations, their gradients, the token convolution's state), parameters and their gradients and the recurrence's states are
+ * fp32, and so are all sums; a result is rounded to T once.  Matrices are token-major as everywhere here, rows b L + t, with pitches in elements;
+ * pointers need only be aligned to an element, and nothing beyond a row's width is read or written.  Gradients of parameters
+ * are summed in a fixed order: the same inputs give the same bits.  `reverse` != 0 lets time run from a sequence's last row to
+ * its first (a block that scans its tokens both ways): the state before the first token is then the one behind the last row.
+ * At most 2^31 - 1 rows.  Workspaces are device scratch of the caller, 16-byte aligned, of at least the bytes that the
+ * _workspace function says (0: may be NULL); their contents need no initialisation and are free once the call's work is done.
+ */
+typedef enum { PTQ4VM_F16 = 0, PTQ4VM_BF16 = 1, PTQ4VM_F32 = 2 } ptq4vm_dtype;
+
+/*
+ * Gated linear recurrence over tokens (the state equations of Sec. 2.1, Eqs. (1)-(8), the input matrix to first order), with its
+ * skip and its gate.  For each sequence, channel k < K and state n < N, in the order of time:
+ *   D = ln(1 + exp(dt[t,k] + dt_bias[k])),  h_t[k,n] = exp(D a[k,n]) h_{t-1}[k,n] + D u[t,k] b[t,n],
+ *   s = sum_n c[t,n] h_t[k,n] + d[k] u[t,k],  y[t,k] = s z[t,k] / (1 + exp(-z[t,k]))
+ *   u, dt [B*L, K], b, c [B*L, N]  T in      the columns of x_proj's output or any other matrix
+ *   a [K, N] f32 in, dense;  d [K], dt_bias [K] f32 in, may be NULL (zeros);  z [B*L, K] T in, may be NULL (no gate: y = s)
+ *   state     [B, K, N] f32 in, dense, may be NULL (zeros): h before the first token
+ *   y         [B*L, K]  T out
+ *   state_out [B, K, N] f32 out, may be NULL: h behind the last token.  Not the buffer of `state`.
+ *   marks     [PTQ4VM_SCAN_MARKS(L), B, K, N] f32 out, may be NULL: h before every PTQ4VM_SCAN_TILE-th token, for the backward
+ *             pass
+ * Few long sequences are cut into chunks that run side by side (two launches).  Errors: NULL u / dt / a / b / c / y, sizes out of
+ * range (N up to PTQ4VM_MAX_SCAN_N), ld* below a row's width, misalignment, workspace too small (PTQ4VM_ERR_SHAPE) or missing.
+ */
+#define PTQ4VM_SCAN_TILE 16
+#define PTQ4VM_SCAN_MARKS(L) ((((int64_t)(L)) + PTQ4VM_SCAN_TILE - 1) / PTQ4VM_SCAN_TILE)
+#define PTQ4VM_MAX_SCAN_N 64
+int64_t ptq4vm_gated_scan_workspace(int64_t B, int64_t L, int64_t K, int64_t N);
+int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d,
+                      const void *z, const float *dt_bias, const float *state, void *y, float *state_out, float *marks,
+                      void *workspace, int64_t workspace_bytes, int reverse, int64_t B, int64_t L, int64_t K, int64_t N,
+                      int64_t ldu, int64_t lddt, int64_t ldb, int64_t ldc, int64_t ldz, int64_t ldy, void *stream);
+
+/*
+ * Its backward pass: the gradients of everything that ptq4vm_gated_scan reads, given the gradient dy of y and the marks that
+ * the forward pass left (they hold its first state too).  States are constants here: no gradient goes into `state` or comes
+ * out of state_out.  Inputs and `reverse` as in the forward call.
+ *   du, ddt, dz [B*L, K], db, dc [B*L, N] T out;  da [K, N], dd [K], ddt_bias [K] f32 out (dd, dz, ddt_bias may be NULL
+ *   where d, z, dt_bias are)
+ * Errors as for ptq4vm_gated_scan.  B = 0 writes zeros to da, dd and ddt_bias.
+ */
+int64_t ptq4vm_gated_scan_backward_workspace(int64_t B, int64_t L, int64_t K, int64_t N);
+int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const void *dt, const float *a, const void *b,
+                               const void *c, const float *d, const void *z, const float *dt_bias, const float *marks, void *du,
+                               void *ddt, float *da, void *db, void *dc, float *dd, void *dz, float *ddt_bias, void *workspace,
+                               int64_t workspace_bytes, int reverse, int64_t B, int64_t L, int64_t K, int64_t N, int64_t lddy,
+                               int64_t ldu, int64_t lddt, int64_t ldb, int64_t ldc, int64_t ldz, int64_t lddu, int64_t ldddt,
+                               int64_t lddb, int64_t lddc, int64_t lddz, void *stream);
+
+/*
+ * One token of each of B sequences: ptq4vm_gated_scan with L = 1 on the states [B, K, N], which it advances.  state_out may be
+ * the buffer of `state` (in place).  Errors as there, and NULL state / state_out.
+ */
+int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d,
+                           const void *z, const float *dt_bias, const float *state, void *y, float *state_out, int64_t B,
+                           int64_t K, int64_t N, int64_t ldu, int64_t lddt, int64_t ldb, int64_t ldc, int64_t ldz, int64_t ldy,
+                           void *stream);
+
+/*
+ * Short convolution over tokens, one filter of W = 2, 3 or 4 taps per channel (between in_proj and x_proj of a block):
+ *   p[t,k] = bias[k] + sum_j w[k,j] x[t - W + 1 + j, k],  y = p / (1 + exp(-p)) where silu != 0, else p
+ *   x [B*L, K] T in, w [K, W] f32 in, dense, bias [K] f32 in, may be NULL
+ *   state     [B, W - 1, K] T in, dense, may be NULL (zeros): x of the W - 1 tokens before the first
+ *   y         [B*L, K] T out
+ *   state_out [B, W - 1, K] T out, may be NULL: x of the last W - 1 tokens (of state's where L < W - 1).  Not the buffer of `state`.
+ * The backward pass gives dx [B*L, K] T, dw [K, W] f32 and dbias [K] f32 (may be NULL) for the gradient dy of y; the state is a
+ * constant.  The step is L = 1 on states that it advances; its state_out may be the buffer of `state`.
+ * Errors: NULL x / w / y (dy / x / w / dx / dw; x / w / state / y / state_out), sizes out of range, ld* < K, misalignment,
+ * workspace too small (PTQ4VM_ERR_SHAPE) or missing.  B = 0 writes zeros to dw and dbias.
+ */
+int ptq4vm_token_conv(int dtype, const void *x, const float *w, const float *bias, const void *state, void *y, void *state_out,
+                      int silu, int reverse, int64_t B, int64_t L, int64_t K, int64_t W, int64_t ldx, int64_t ldy, void *stream);
+int64_t ptq4vm_token_conv_backward_workspace(int64_t B, int64_t L, int64_t K, int64_t W);
+int ptq4vm_token_conv_backward(int dtype, const void *dy, const void *x, const float *w, const float *bias, const void *state,
+                               void *dx, float *dw, float *dbias, void *workspace, int64_t workspace_bytes, int silu, int reverse,
+                               int64_t B, int64_t L, int64_t K, int64_t W, int64_t lddy, int64_t ldx, int64_t lddx, void *stream);
+int ptq4vm_token_conv_step(int dtype, const void *x, const float *w, const float *bias, const void *state, void *y,
+                           void *state_out, int silu, int64_t B, int64_t K, int64_t W, int64_t ldx, int64_t ldy, void *stream);
+
+/*
+ * The norms after and before a block, with the block's gate and the residual stream between them:
+ *   q = norm(h) w_post (or h),  r = scale residual + gate q,  y = norm(r) w,  norm(v) = v / sqrt(mean_k v^2 + eps)
+ *   h        [M, K] T in    the block's output;  y [M, K] T out, the next block's input
+ *   residual [M, K] in, may be NULL (zeros: the first block);  r [M, K] out.  Both of type stream_dtype: T or fp32
+ *   w [K], w_post [K] f32 in; w_post may be NULL (no norm after the block)
+ *   gate     [G, K] f32 in, dense, may be NULL (ones): row i takes gate row i / (M / G), so G = 1 is a gate per channel, G = B one
+ *            per image, G = M one per token
+ * y is computed from r before it is rounded to stream_dtype.  The backward pass takes h and r, the gradient dy of y and the
+ * gradient dr of r from the blocks behind (may be NULL: zeros) and gives dh [M, K] T, dresidual [M, K] stream_dtype (may be NULL),
+ * dw [K], dgate [G, K] and dw_post [K] f32.
+ * Errors: NULL h / w / y / r (dy / h / r / w / dh / dw, and dgate, dw_post with their inputs), sizes out of range (K up to
+ * PTQ4VM_MAX_NORM_K, G that does not divide M), a stream_dtype that is neither, ld* < K, misalignment, workspace too small
+ * (PTQ4VM_ERR_SHAPE) or missing.  M = 0 writes zeros to dw, dgate and dw_post.  G of the workspace function is 0 without a gate.
+ */
+#define PTQ4VM_MAX_NORM_K 16384
+int ptq4vm_residual_norm(int dtype, int stream_dtype, const void *h, const void *residual, const float *w, const float *gate,
+                         const float *w_post, void *y, void *r, float scale, float eps, int64_t M, int64_t K, int64_t G,
+                         int64_t ldh, int64_t ldres, int64_t ldy, int64_t ldr, void *stream);
+int64_t ptq4vm_residual_norm_backward_workspace(int64_t M, int64_t K, int64_t G);
+int ptq4vm_residual_norm_backward(int dtype, int stream_dtype, const void *dy, const void *dr, const void *h, const void *r,
+                                  const float *w, const float *gate, const float *w_post, void *dh, void *dresidual, float *dw,
+                                  float *dgate, float *dw_post, void *workspace, int64_t workspace_bytes, float scale, float eps,
+                                  int64_t M, int64_t K, int64_t G, int64_t lddy, int64_t lddr, int64_t ldh, int64_t ldr,
+                                  int64_t lddh, int64_t lddres, void *stream);
+
 /* Static, never freed. */
 const char *ptq4vm_status_string(int status);
 /* Thread-local text of the last HIP error that produced PTQ4VM_ERR_HIP on this thread. */

@@ -1,4 +1,4 @@
-"""MI355X-native PTQ4VM quantized-linear path (arXiv 2412.20386).
+"""MI355X-native PTQ4VM quantized-linear path and the operators between a block's linears (arXiv 2412.20386).
 
 `binding` exposes the C ABI of libptq4vm.so (hand-written HIP for gfx950); `synth` draws the
 seeded Vim-shaped inputs; `build` compiles the library.  Importing the package loads the extension
@@ -26,6 +26,15 @@ from .binding import (  # noqa: F401
     w8a8_linear_offset_fused,
     w8a8_linear,
     w8a8_linear_fused,
+    gated_scan,
+    gated_scan_backward,
+    gated_scan_step,
+    scan_marks,
+    token_conv,
+    token_conv_backward,
+    token_conv_step,
+    residual_norm,
+    residual_norm_backward,
     validate_scales,
     validate_scales_static,
 )

@@ -5,7 +5,7 @@ pointers, sizes and the current HIP stream to the C ABI declared in include/ptq4
 returns the output tensors.  No arithmetic happens here and there is no fallback: if the
 library has not been built, loading raises.
 
-The launches of the hot path (quantizers and linears) are callables of the extension module
+The launches of the hot path (quantizers, linears and the operators between them) are callables of the extension module
 _calls (host/calls.cc), which does the same checks natively; the offline preparation of weights
 and the validator go through ctypes here.
 """
@@ -45,6 +45,18 @@ EXPORTS = (
     "ptq4vm_f16_linear",
     "ptq4vm_validate_scales",
     "ptq4vm_validate_scales_static",
+    "ptq4vm_gated_scan",
+    "ptq4vm_gated_scan_workspace",
+    "ptq4vm_gated_scan_backward",
+    "ptq4vm_gated_scan_backward_workspace",
+    "ptq4vm_gated_scan_step",
+    "ptq4vm_token_conv",
+    "ptq4vm_token_conv_backward",
+    "ptq4vm_token_conv_backward_workspace",
+    "ptq4vm_token_conv_step",
+    "ptq4vm_residual_norm",
+    "ptq4vm_residual_norm_backward",
+    "ptq4vm_residual_norm_backward_workspace",
     "ptq4vm_status_string",
     "ptq4vm_last_hip_error",
     "ptq4vm_version",
@@ -104,6 +116,22 @@ def load() -> ctypes.CDLL:
                                              i64, vp]
     lib.ptq4vm_f16_linear.restype = ci
     lib.ptq4vm_f16_linear.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, vp]
+    cf = ctypes.c_float
+    for name, argtypes in {
+        "gated_scan": [ci] + [vp] * 13 + [i64, ci] + [i64] * 10 + [vp],
+        "gated_scan_backward": [ci] + [vp] * 19 + [i64, ci] + [i64] * 15 + [vp],
+        "gated_scan_step": [ci] + [vp] * 11 + [i64] * 9 + [vp],
+        "token_conv": [ci] + [vp] * 6 + [ci] * 2 + [i64] * 6 + [vp],
+        "token_conv_backward": [ci] + [vp] * 9 + [i64] + [ci] * 2 + [i64] * 7 + [vp],
+        "token_conv_step": [ci] + [vp] * 6 + [ci] + [i64] * 5 + [vp],
+        "residual_norm": [ci] * 2 + [vp] * 7 + [cf] * 2 + [i64] * 7 + [vp],
+        "residual_norm_backward": [ci] * 2 + [vp] * 13 + [i64] + [cf] * 2 + [i64] * 9 + [vp],
+    }.items():
+        getattr(lib, "ptq4vm_" + name).restype = ci
+        getattr(lib, "ptq4vm_" + name).argtypes = argtypes
+    for name, sizes in {"gated_scan": 4, "gated_scan_backward": 4, "token_conv_backward": 4, "residual_norm_backward": 3}.items():
+        getattr(lib, f"ptq4vm_{name}_workspace").restype = i64
+        getattr(lib, f"ptq4vm_{name}_workspace").argtypes = [i64] * sizes
     lib.ptq4vm_validate_scales.restype = ci
     lib.ptq4vm_validate_scales.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, i64, vp]
     lib.ptq4vm_validate_scales_static.restype = ci
@@ -121,13 +149,16 @@ def load() -> ctypes.CDLL:
 # ---------------------------------------------------------------------------------- launches of the hot path
 HOT_CALLS = ("quantize_pts", "quantize_dynamic", "quantize_pts_offset", "quantize_pts_a4", "quantize_pts_a4_e2m3",
              "w8a8_linear", "w8a8_linear_offset", "w4a4_linear", "w4a4_linear_e2m3", "w8a8_linear_fused",
-             "w8a8_linear_offset_fused", "w4a4_linear_fused", "f16_linear")
+             "w8a8_linear_offset_fused", "w4a4_linear_fused", "f16_linear",
+             "gated_scan", "gated_scan_backward", "gated_scan_step", "token_conv", "token_conv_backward", "token_conv_step",
+             "residual_norm", "residual_norm_backward")
+_WORKSPACES = ("gated_scan_workspace", "gated_scan_backward_workspace", "token_conv_backward_workspace", "residual_norm_backward_workspace")
 
 
 def _load_entries() -> None:
     """Hand the library's entry points to _calls (its callables ask for this on their first call)."""
     lib = load()
-    _calls.bind({name: ctypes.cast(getattr(lib, "ptq4vm_" + name), ctypes.c_void_p).value for name in HOT_CALLS})
+    _calls.bind({name: ctypes.cast(getattr(lib, "ptq4vm_" + name), ctypes.c_void_p).value for name in HOT_CALLS + _WORKSPACES})
 
 
 _BUILD_HINT = "build it with `python -m paper_2412_20386_amd.build` (there is no CPU or PyTorch fallback)"
@@ -247,6 +278,14 @@ def fold_smoothing_w4(w: torch.Tensor, m: torch.Tensor, wq4: Optional[torch.Tens
 def e2m3_blocks(K: int) -> int:
     """PTQ4VM_E2M3_BLOCKS: 96-byte blocks of 128 codes that a row of K codes takes in the E2M3 container."""
     return (K + 127) // 128
+
+
+SCAN_TILE = 16  # PTQ4VM_SCAN_TILE
+
+
+def scan_marks(L: int) -> int:
+    """PTQ4VM_SCAN_MARKS: states that gated_scan keeps of a sequence of L tokens for its backward pass."""
+    return (L + SCAN_TILE - 1) // SCAN_TILE
 
 
 def _e2m3_container(t: torch.Tensor, rows: int, K: int, what: str) -> int:

@@ -1,0 +1,269 @@
+// Forward pass of the gated linear recurrence (gated_scan.hpp has the formulas and the layout), and its form for one token.
+#include "gated_scan.hpp"
+
+namespace {
+
+using namespace ptq4vm;
+
+// One wavefront: 16 C channels of one sequence through the tokens of one chunk.
+// STATES_ONLY: from a zero state, without outputs; leaves the chunk's end state and its sum of D, from which the chunks behind
+// it know their first state: h_in(i + 1) = exp(a sum D(i)) h_in(i) + h_end(i).
+// PADDED: N is no multiple of what a quad holds; the states behind N are kept at zero.
+template <typename T, int NS, int C, bool PADDED, bool STATES_ONLY>
+__global__ __launch_bounds__(64) void gated_scan_tokens(ScanArgs<T> p) {
+    using S = ScanLane<NS, C>;
+    __shared__ float2 steps[kTile][S::kChannels];  // D and D u
+    __shared__ float sums[kTile][S::kChannels];    // s without its d u
+    __shared__ float sb[kTile][S::kStates], sc[kTile][S::kStates];
+    const uint32_t block = xcd_contiguous(blockIdx.x, p.blocks);
+    if (block >= p.blocks) return;
+    const int cb = block % p.column_blocks, bc = block / p.column_blocks, b = bc % p.B;
+    const uint32_t chunk = bc / p.B;
+    const int lane = threadIdx.x, q = lane & 3, cl = lane >> 2, n0 = q * NS;
+    const int64_t t_begin = chunk * p.chunk_tokens, t_end = min(p.L, t_begin + p.chunk_tokens);
+
+    float a2[C][NS], h[C][NS], sum_d[C];
+#pragma unroll
+    for (int c = 0; c < C; c++) {
+        const int k = cb * S::kChannels + cl * C + c, n = k < p.K ? p.N : 0;
+        const int64_t at = ((int64_t)b * p.K + k) * p.N;
+        load_channel<NS>(p.a + (int64_t)(k < p.K ? k : 0) * p.N, n0, n, a2[c]);
+        sum_d[c] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NS; i++) a2[c][i] *= kLog2e, h[c][i] = 0.0f;
+        if constexpr (!STATES_ONLY) {
+            if (p.state) load_channel<NS>(p.state + (n ? at : 0), n0, n, h[c]);
+            for (uint32_t i = 0; i < chunk; i++) {
+                const int64_t from = (int64_t)i * p.B * p.K;
+                float end[NS];
+                load_channel<NS>(p.chunk_state + (n ? from * p.N + at : 0), n0, n, end);
+                const float D = n ? p.chunk_dt[from + (int64_t)b * p.K + k] : 0.0f;
+#pragma unroll
+                for (int j = 0; j < NS; j++) h[c][j] = fmaf(__builtin_amdgcn_exp2f(a2[c][j] * D), h[c][j], end[j]);
+            }
+        }
+    }
+
+    // what this lane loads: kVec channels of a token
+    const int vt = lane / S::kAcross, vk = (lane % S::kAcross) * S::kVec, k = cb * S::kChannels + vk, nk = max(0, min(S::kVec, p.K - k));
+    float bias[S::kVec], skip[S::kVec];
+#pragma unroll
+    for (int i = 0; i < S::kVec; i++) {
+        bias[i] = p.dt_bias && i < nk ? p.dt_bias[k + i] : 0.0f;
+        skip[i] = !STATES_ONLY && p.d && i < nk ? p.d[k + i] : 0.0f;
+    }
+    T ru[S::kPasses][S::kVec], rdt[S::kPasses][S::kVec], rz[S::kPasses][S::kVec], rb[NS], rc[NS];
+    const auto fetch = [&](int64_t t0) {
+#pragma unroll
+        for (int s = 0; s < S::kPasses; s++) {
+            const int64_t t = t0 + s * S::kTokens + vt;
+            const int n = t < t_end ? nk : 0;
+            load_first<S::kVec>(p.u.at(b, n ? t : 0) + k, n, ru[s]);
+            load_first<S::kVec>(p.dt.at(b, n ? t : 0) + k, n, rdt[s]);
+            if (!STATES_ONLY && p.z.data) load_first<S::kVec>(p.z.at(b, n ? t : 0) + k, n, rz[s]);
+        }
+        load_states<NS>(p.b, b, t0, t_end, p.N, rb);
+        if constexpr (!STATES_ONLY) load_states<NS>(p.c, b, t0, t_end, p.N, rc);
+    };
+    fetch(t_begin);
+    for (int64_t t0 = t_begin; t0 < t_end; t0 += kTile) {
+        T u[S::kPasses][S::kVec], z[S::kPasses][S::kVec];
+#pragma unroll
+        for (int s = 0; s < S::kPasses; s++) {
+            const bool there = t0 + s * S::kTokens + vt < t_end;  // (tokens behind the last change nothing: D = 0)
+#pragma unroll
+            for (int i = 0; i < S::kVec; i++) {
+                u[s][i] = ru[s][i];
+                if (!STATES_ONLY) z[s][i] = rz[s][i];
+                const float D = there ? softplus_of((float)rdt[s][i] + bias[i]) : 0.0f;
+                steps[s * S::kTokens + vt][vk + i] = {D, there ? D * (float)ru[s][i] : 0.0f};
+            }
+        }
+        keep_states<NS>(rb, sb);
+        if constexpr (!STATES_ONLY) keep_states<NS>(rc, sc);
+        __syncthreads();
+        if (t0 + kTile < t_end) fetch(t0 + kTile);  // in flight under this tile's steps
+        if (!STATES_ONLY && p.marks)
+#pragma unroll
+            for (int c = 0; c < C; c++) {
+                const int kc = cb * S::kChannels + cl * C + c;
+                if (kc < p.K) store_channel<NS>(p.marks + (((t0 / kTile) * p.B + b) * p.K + kc) * p.N, n0, p.N, h[c]);
+            }
+        const int groups = (int)((min((int64_t)kTile, t_end - t0) + 3) / 4);
+        for (int g = 0; g < groups; g++)
+#pragma unroll
+            for (int s = 0; s < 4; s++) {
+                const int t = 4 * g + s;
+                float B[NS], CC[NS], v[C];
+#pragma unroll
+                for (int i = 0; i < NS; i++) {
+                    B[i] = sb[t][n0 + i];
+                    if (!STATES_ONLY) CC[i] = sc[t][n0 + i];
+                }
+#pragma unroll
+                for (int c = 0; c < C; c++) {
+                    const float2 D = steps[t][cl * C + c];
+                    v[c] = 0.0f;
+                    if (STATES_ONLY) sum_d[c] += D.x;
+#pragma unroll
+                    for (int i = 0; i < NS; i++) {
+                        h[c][i] = fmaf(__builtin_amdgcn_exp2f(a2[c][i] * D.x), h[c][i], D.y * B[i]);
+                        if (PADDED) h[c][i] = n0 + i < p.N ? h[c][i] : 0.0f;
+                        if (!STATES_ONLY) v[c] = fmaf(h[c][i], CC[i], v[c]);
+                    }
+                    if (!STATES_ONLY) v[c] = quad_sum(v[c]);
+                }
+                if constexpr (!STATES_ONLY)
+                    if (q < C) sums[t][cl * C + q] = C == 2 && q == 1 ? v[C - 1] : v[0];
+            }
+        __syncthreads();
+        if constexpr (!STATES_ONLY)
+#pragma unroll
+            for (int s = 0; s < S::kPasses; s++) {
+                const int64_t t = t0 + s * S::kTokens + vt;
+                float y[S::kVec];
+#pragma unroll
+                for (int i = 0; i < S::kVec; i++) {
+                    y[i] = fmaf(skip[i], (float)u[s][i], sums[s * S::kTokens + vt][vk + i]);
+                    if (p.z.data) y[i] *= (float)z[s][i] * sigmoid_of((float)z[s][i]);
+                }
+                if (t < t_end && nk) store_first<S::kVec>(p.y.at(b, t) + k, nk, y);
+            }
+    }
+    float *const out = STATES_ONLY ? p.chunk_state + (int64_t)chunk * p.B * p.K * p.N : t_end == p.L ? p.state_out : nullptr;
+    if (out)
+#pragma unroll
+        for (int c = 0; c < C; c++) {
+            const int kc = cb * S::kChannels + cl * C + c;
+            if (kc < p.K) store_channel<NS>(out + ((int64_t)b * p.K + kc) * p.N, n0, p.N, h[c]);
+            if (STATES_ONLY && kc < p.K && q == 0) p.chunk_dt[((int64_t)chunk * p.B + b) * p.K + kc] = sum_d[c];
+        }
+}
+
+// One token of every sequence: bound by the states, which are read and written once (128 bytes of a channel's 16 against 10
+// of everything else).  A quad of lanes takes a channel, its lanes adjacent states.  A lane's states are read before they are
+// written by it alone, so state_out may be the state's own buffer.
+template <typename T, int NS>
+__global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 2;
+    const int q = threadIdx.x & 3, n0 = q * NS;
+    const bool there = at < (int64_t)p.B * p.K;
+    const int64_t ch = there ? at : 0;
+    const int b = (int)(ch / p.K), k = (int)(ch - (int64_t)b * p.K);
+    float h[NS], a[NS];
+    T B[NS], CC[NS];
+    const int n = max(0, min(NS, p.N - n0));
+    load_channel<NS>(p.state + ch * p.N, n0, p.N, h);
+    load_channel<NS>(p.a + (int64_t)k * p.N, n0, p.N, a);
+    load_first<NS>(p.b.at(b, 0) + n0, n, B);
+    load_first<NS>(p.c.at(b, 0) + n0, n, CC);
+    const float u = (float)p.u.at(b, 0)[k];
+    const float D = softplus_of((float)p.dt.at(b, 0)[k] + (p.dt_bias ? p.dt_bias[k] : 0.0f)), Du = D * u;
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NS; i++) {
+        h[i] = fmaf(__builtin_amdgcn_exp2f(a[i] * kLog2e * D), h[i], Du * (float)B[i]);
+        v = i < n ? fmaf(h[i], (float)CC[i], v) : v;
+    }
+    v = quad_sum(v);
+    if (!there) return;
+    store_channel<NS>(p.state_out + ch * p.N, n0, p.N, h);
+    if (q != 0) return;
+    if (p.d) v = fmaf(p.d[k], u, v);
+    if (p.z.data) {
+        const float z = (float)p.z.at(b, 0)[k];
+        v *= z * sigmoid_of(z);
+    }
+    p.y.at(b, 0)[k] = (T)v;
+}
+
+int check_scan(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d, const void *z, const float *dt_bias, void *y,
+               int64_t B, int64_t L, int64_t K, int64_t N, int64_t ldu, int64_t lddt, int64_t ldb, int64_t ldc, int64_t ldz, int64_t ldy) {
+    if (!valid_dtype(dtype)) return PTQ4VM_ERR_SHAPE;
+    if (!a || (B != 0 && (!u || !dt || !b || !c || !y))) return PTQ4VM_ERR_NULL;  // (a matrix of no rows has no address)
+    if (!scan_sizes(B, L, K, N)) return PTQ4VM_ERR_SHAPE;
+    if (ldu < K || lddt < K || ldb < N || ldc < N || (z && ldz < K) || ldy < K) return PTQ4VM_ERR_STRIDE;
+    const uintptr_t e = dtype_bytes(dtype);
+    if (!aligned_to(u, e) || !aligned_to(dt, e) || !aligned_to(b, e) || !aligned_to(c, e) || !aligned_to(z, e) || !aligned_to(y, e) || !aligned_to(a, 4) ||
+        !aligned_to(d, 4) || !aligned_to(dt_bias, 4))
+        return PTQ4VM_ERR_ALIGN;
+    return PTQ4VM_OK;
+}
+
+template <typename T>
+ScanArgs<T> scan_args(const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d, const void *z, const float *dt_bias, void *y,
+                      bool reverse, int64_t B, int64_t L, int64_t K, int64_t N, int64_t ldu, int64_t lddt, int64_t ldb, int64_t ldc, int64_t ldz, int64_t ldy) {
+    ScanArgs<T> s{};
+    s.u = tokens<T>(u, L, ldu, reverse), s.dt = tokens<T>(dt, L, lddt, reverse), s.b = tokens<T>(b, L, ldb, reverse), s.c = tokens<T>(c, L, ldc, reverse);
+    s.z = tokens<T>(z, L, ldz, reverse), s.y = tokens<T>(y, L, ldy, reverse);
+    s.a = a, s.d = d, s.dt_bias = dt_bias, s.B = (int)B, s.K = (int)K, s.N = (int)N, s.L = L;
+    return s;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t ptq4vm_gated_scan_workspace(int64_t B, int64_t L, int64_t K, int64_t N) {
+    if (!scan_sizes(B, L, K, N) || B == 0) return 0;
+    const ScanPlan plan = scan_plan(B, L, K, N);
+    return plan.chunks > 1 ? plan.chunks * B * K * (N + 1) * 4 : 0;
+}
+
+int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d, const void *z, const float *dt_bias,
+                      const float *state, void *y, float *state_out, float *marks, void *workspace, int64_t workspace_bytes, int reverse, int64_t B, int64_t L, int64_t K,
+                      int64_t N, int64_t ldu, int64_t lddt, int64_t ldb, int64_t ldc, int64_t ldz, int64_t ldy, void *stream_) {
+    const int rc = check_scan(dtype, u, dt, a, b, c, d, z, dt_bias, y, B, L, K, N, ldu, lddt, ldb, ldc, ldz, ldy);
+    if (rc != PTQ4VM_OK) return rc;
+    const int64_t need = ptq4vm_gated_scan_workspace(B, L, K, N);
+    if (need > 0 && !workspace) return PTQ4VM_ERR_NULL;
+    if (workspace_bytes < need) return PTQ4VM_ERR_SHAPE;
+    if (!aligned_to(state, 4) || !aligned_to(state_out, 4) || !aligned_to(marks, 4) || (need > 0 && !aligned_to(workspace, 16))) return PTQ4VM_ERR_ALIGN;
+    if (B == 0) return PTQ4VM_OK;
+    const ScanPlan plan = scan_plan(B, L, K, N);
+    hipStream_t stream = static_cast<hipStream_t>(stream_);
+    return for_dtype(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        ScanArgs<T> s = scan_args<T>(u, dt, a, b, c, d, z, dt_bias, y, reverse, B, L, K, N, ldu, lddt, ldb, ldc, ldz, ldy);
+        s.state = state, s.state_out = state_out, s.marks = marks;
+        s.chunk_state = static_cast<float *>(workspace), s.chunk_dt = s.chunk_state + (plan.chunks > 1 ? plan.chunks * B * K * N : 0);
+        s.column_blocks = (int)plan.column_blocks, s.chunk_tokens = plan.chunk_tokens;
+        return for_layout(plan, N, [&](auto ns, auto ch, auto padded) {
+            const auto go = [&](auto states_only, int64_t chunks) {
+                s.chunks = (uint32_t)chunks, s.blocks = (uint32_t)(chunks * B * plan.column_blocks);
+                gated_scan_tokens<T, ns(), ch(), padded(), states_only()><<<dim3(xcd_grid(s.blocks)), dim3(64), 0, stream>>>(s);
+                return check_launch("gated_scan_tokens");
+            };
+            if (plan.chunks > 1)  // (nobody asks for the last chunk's)
+                if (const int e = go(std::true_type{}, plan.chunks - 1)) return e;
+            return go(std::false_type{}, plan.chunks);
+        });
+    });
+}
+
+int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d, const void *z, const float *dt_bias,
+                           const float *state, void *y, float *state_out, int64_t B, int64_t K, int64_t N, int64_t ldu, int64_t lddt, int64_t ldb, int64_t ldc,
+                           int64_t ldz, int64_t ldy, void *stream_) {
+    const int rc = check_scan(dtype, u, dt, a, b, c, d, z, dt_bias, y, B, 1, K, N, ldu, lddt, ldb, ldc, ldz, ldy);
+    if (rc != PTQ4VM_OK) return rc;
+    if (B != 0 && (!state || !state_out)) return PTQ4VM_ERR_NULL;
+    if (!aligned_to(state, 4) || !aligned_to(state_out, 4)) return PTQ4VM_ERR_ALIGN;
+    if (B == 0) return PTQ4VM_OK;
+    const int64_t blocks = ceil_div(B * K, 64);
+    if (blocks > kMaxTokenRows) return PTQ4VM_ERR_SHAPE;
+    hipStream_t stream = static_cast<hipStream_t>(stream_);
+    return for_dtype(dtype, [&](auto zero) {
+        using T = decltype(zero);
+        ScanArgs<T> s = scan_args<T>(u, dt, a, b, c, d, z, dt_bias, y, false, B, 1, K, N, ldu, lddt, ldb, ldc, ldz, ldy);
+        s.state = state, s.state_out = state_out;
+        const dim3 grid((unsigned)blocks);
+        switch (states_per_lane(N)) {
+            case 1: gated_scan_one_token<T, 1><<<grid, dim3(256), 0, stream>>>(s); break;
+            case 4: gated_scan_one_token<T, 4><<<grid, dim3(256), 0, stream>>>(s); break;
+            default: gated_scan_one_token<T, 16><<<grid, dim3(256), 0, stream>>>(s); break;
+        }
+        return check_launch("gated_scan_one_token");
+    });
+}
+
+}  // extern "C"

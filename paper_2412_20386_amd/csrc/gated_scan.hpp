@@ -1,0 +1,113 @@
+// The gated linear recurrence over tokens: what its kernels share.  For one sequence, channel k and state n:
+//   D = softplus(dt + dt_bias),  h_t = exp(D a[k,n]) h_{t-1} + D u b[t,n],  s = sum_n c[t,n] h_t + d[k] u,  y = s z / (1 + e^-z)
+// (the state equations of Sec. 2.1 with the input matrix to first order, Eqs. (1)-(8); u, dt, z and y have K columns, b and c
+// have N, shared by all channels).
+//
+// A quad of lanes holds the states of C channels, NS of each to a lane, so that a wavefront runs 16 C channels through the
+// tokens with the states in registers, sums over n are two DPP additions, and what belongs to a token and channel (softplus,
+// gate) is computed once, by the lane that loaded it, and passed through LDS.  Bound by the vector ALU: a token, channel and
+// state cost one exponential and four other instructions, against 8 bytes for all states of a channel.
+#pragma once
+#include <type_traits>
+
+#include "token_ops.hpp"
+
+namespace ptq4vm {
+
+constexpr int kTile = PTQ4VM_SCAN_TILE;  // tokens that are staged together; marks are kept for their starts
+
+template <typename T>
+struct ScanArgs {
+    Tokens<T> u, dt, b, c, z, y;
+    const float *a, *d, *dt_bias, *state;
+    float *state_out, *marks;
+    float *chunk_state, *chunk_dt;  // [chunks][B][K][N] and [chunks][B][K]: a chunk's own end state and its sum of D
+    // backward
+    Tokens<T> dy, du, ddt, dz;
+    float *partial_bc, *partial_a;
+    int B, K, N, column_blocks;
+    int64_t L, chunk_tokens;  // (a multiple of kTile)
+    uint32_t chunks, blocks;
+};
+
+// What the layout of a wavefront makes of its lane number
+template <int NS, int C>
+struct ScanLane {
+    static constexpr int kChannels = 16 * C;             // of a wavefront
+    static constexpr int kStates = 4 * NS;               // that a quad has room for
+    static constexpr int kVec = C == 1 ? 4 : 8;          // channels that a lane loads of one token
+    static constexpr int kAcross = kChannels / kVec;     // lanes side by side
+    static constexpr int kTokens = 64 / kAcross;         // tokens that a wavefront loads at once
+    static constexpr int kPasses = kTile / kTokens;
+};
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// Channels and states of the kernels' variants: states in quads of 1, 4 or 16 each, two channels to a lane where that leaves
+// two wavefronts to a SIMD
+inline int states_per_lane(int64_t N) { return N <= 4 ? 1 : N <= 16 ? 4 : 16; }
+inline int channels_per_lane(int64_t B, int64_t K, int64_t N) { return N <= 16 && B * ceil_div(K, 32) >= 2048 ? 2 : 1; }
+
+// Chunks of a sequence: one unless that leaves the device half empty, then as many as fill it, of two tiles at least
+struct ScanPlan {
+    int channels, states;
+    int64_t column_blocks, chunk_tokens, chunks;
+};
+inline ScanPlan scan_plan(int64_t B, int64_t L, int64_t K, int64_t N) {
+    ScanPlan p{channels_per_lane(B, K, N), states_per_lane(N), 0, 0, 0};
+    p.column_blocks = ceil_div(K, 16 * p.channels);
+    const int64_t waves = B * p.column_blocks;
+    int64_t chunks = waves >= 1024 ? 1 : ceil_div(2048, waves > 0 ? waves : 1);
+    if (chunks > ceil_div(L, 2 * kTile)) chunks = ceil_div(L, 2 * kTile);
+    if (chunks > 64) chunks = 64;
+    p.chunk_tokens = ceil_div(ceil_div(L, chunks), kTile) * kTile;
+    p.chunks = ceil_div(L, p.chunk_tokens);
+    return p;
+}
+
+template <typename F>
+int for_layout(const ScanPlan &p, int64_t N, F &&f) {
+    using std::bool_constant;
+    using std::integral_constant;
+    const auto with = [&](auto ns, auto c) { return N == 4 * ns() ? f(ns, c, bool_constant<false>{}) : f(ns, c, bool_constant<true>{}); };
+    if (p.states == 16) return with(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    if (p.channels == 2) return p.states == 4 ? with(integral_constant<int, 4>{}, integral_constant<int, 2>{}) : with(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+    return p.states == 4 ? with(integral_constant<int, 4>{}, integral_constant<int, 1>{}) : with(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+}
+
+// Sizes that every entry point takes
+inline bool scan_sizes(int64_t B, int64_t L, int64_t K, int64_t N) {
+    return B >= 0 && L > 0 && K > 0 && N > 0 && N <= PTQ4VM_MAX_SCAN_N && L <= kMaxTokenRows && K <= kMaxTokenRows / 256 && (B == 0 || B <= kMaxTokenRows / L) &&
+           B * ceil_div(K, 16) <= kMaxTokenRows / 64;
+}
+
+// b or c of one tile, as the lanes of a wavefront load it and keep it in LDS: [kTile][kStates] floats, zero behind N and
+// behind the last token
+template <int NS, typename T>
+__device__ __forceinline__ void load_states(const Tokens<T> &v, int b, int64_t t0, int64_t t1, int N, T (&raw)[NS]) {
+#pragma unroll
+    for (int i = 0; i < NS; i++) {
+        const int at = i * 64 + (threadIdx.x & 63), t = at / (4 * NS), n = at % (4 * NS);
+        raw[i] = t0 + t < t1 && n < N ? v.at(b, t0 + t)[n] : (T)0.0f;
+    }
+}
+template <int NS, typename T>
+__device__ __forceinline__ void keep_states(const T (&raw)[NS], float (*to)[4 * NS]) {
+#pragma unroll
+    for (int i = 0; i < NS; i++) {
+        const int at = i * 64 + (threadIdx.x & 63);
+        to[at / (4 * NS)][at % (4 * NS)] = (float)raw[i];
+    }
+}
+
+// NS states of one channel in a [.., K, N] array
+template <int NS>
+__device__ __forceinline__ void load_channel(const float *p, int n0, int N, float (&v)[NS]) {
+    load_first<NS>(p + n0, max(0, min(NS, N - n0)), v);
+}
+template <int NS>
+__device__ __forceinline__ void store_channel(float *p, int n0, int N, const float (&v)[NS]) {
+    store_first<NS>(p + n0, max(0, min(NS, N - n0)), v);
+}
+
+}  // namespace ptq4vm

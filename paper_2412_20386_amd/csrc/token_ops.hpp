@@ -1,0 +1,149 @@
+// Shared by the operators between a block's linears (gated_scan, token_conv, residual_norm): element types, vectors of
+// elements at any alignment, the activations, and the sum over the partial results of workgroups.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.hpp"
+
+namespace ptq4vm {
+
+constexpr int64_t kMaxTokenRows = 0x7fffffff;  // rows and widths are 32-bit in the kernels, offsets 64-bit
+
+inline bool valid_dtype(int dtype) { return dtype == PTQ4VM_F16 || dtype == PTQ4VM_BF16 || dtype == PTQ4VM_F32; }
+inline uintptr_t dtype_bytes(int dtype) { return dtype == PTQ4VM_F32 ? 4 : 2; }
+
+// f(zero of the element type) for a dtype that valid_dtype() took
+template <typename F>
+int for_dtype(int dtype, F &&f) {
+    if (dtype == PTQ4VM_F16) return f(_Float16{});
+    if (dtype == PTQ4VM_BF16) return f(__bf16{});
+    return f(float{});
+}
+
+// Tokens of a sequence in the order of time: row b * L + t, or b * L + (L - 1 - t) where time runs backwards.
+template <typename T>
+struct Tokens {
+    T *data;         // token 0 of sequence 0
+    int64_t token;   // elements to the next token
+    int64_t sequence;
+    __host__ __device__ __forceinline__ T *at(int b, int64_t t) const { return data + b * sequence + t * token; }
+};
+template <typename T>
+inline Tokens<T> tokens(const void *p, int64_t L, int64_t ld, bool reverse) {
+    T *data = static_cast<T *>(const_cast<void *>(p));
+    if (!p) return {nullptr, 0, 0};
+    return {reverse ? data + (L - 1) * ld : data, reverse ? -ld : ld, L * ld};
+}
+
+// Workgroups go to the 8 XCDs in turn, and each XCD has an L2 of its own: work that shares lines or operands gets
+// consecutive numbers, and an XCD a consecutive range of them.  Some numbers are beyond `total`: the caller leaves.
+__device__ __forceinline__ uint32_t xcd_contiguous(uint32_t block, uint32_t total) {
+    return (block & 7) * ((total + 7) >> 3) + (block >> 3);
+}
+inline uint32_t xcd_grid(int64_t total) { return (uint32_t)((total + 7) & ~(int64_t)7); }
+
+// V elements from p, aligned to an element only (gfx950 loads and stores 16 bytes at any alignment of 2 or 4)
+template <int V, typename T>
+__device__ __forceinline__ void load_whole(const T *p, T (&v)[V]) {
+    __builtin_memcpy(v, p, sizeof(v));
+}
+// The first n of V elements, zero behind them: nothing beyond a row's width is read
+template <int V, typename T>
+__device__ __forceinline__ void load_first(const T *p, int n, T (&v)[V]) {
+    if (n >= V) return load_whole<V>(p, v);
+#pragma unroll
+    for (int i = 0; i < V; i++) v[i] = i < n ? p[i] : (T)0.0f;
+}
+template <int V, typename T>
+__device__ __forceinline__ void store_first(T *p, int n, const float (&v)[V]) {
+    T out[V];
+#pragma unroll
+    for (int i = 0; i < V; i++) out[i] = (T)v[i];  // to nearest even, once
+    if (n >= V) {
+        __builtin_memcpy(p, out, sizeof(out));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < V; i++)
+        if (i < n) p[i] = out[i];
+}
+
+// e^v with the hardware's 2^v (1 ulp); the product's rounding is relative to v: |v| <= 16 costs 2^-20 of the result
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896340736f); }
+// 1 / (1 + e^-v): 0 and 1 at the infinities, NaN for a NaN
+__device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-v)); }
+
+// ln(1 + e^v) = max(v, 0) + ln(1 + e), e = e^-|v| in [0, 1], and ln(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3: a series in
+// s^2 <= 1/9 whose first left-out term is 9^-8 / 17 = 1.4e-9 of the result.  No step cancels, so small results (a step size of
+// 0.001 is an input of -7) keep all their digits; ln(1 + e) itself would keep 14 bits of them.
+__device__ __forceinline__ float softplus_of(float v) {
+    const float e = exp_of(-fabsf(v));
+    const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
+    float p = 1.0f / 15;
+    p = fmaf(p, q, 1.0f / 13);
+    p = fmaf(p, q, 1.0f / 11);
+    p = fmaf(p, q, 1.0f / 9);
+    p = fmaf(p, q, 1.0f / 7);
+    p = fmaf(p, q, 1.0f / 5);
+    p = fmaf(p, q, 1.0f / 3);
+    p = fmaf(p, q, 1.0f);
+    return fmaf(s + s, p, fmaxf(v, 0.0f));
+}
+
+// v + v of another lane of the row of 16, a VALU instruction
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// Sum over the 4 lanes of a quad, in every lane of it
+__device__ __forceinline__ float quad_sum(float v) { return add_dpp<0x4E>(add_dpp<0xB1>(v)); }
+// Sum over an aligned group of `lanes` = 2^n lanes, in every lane of it
+__device__ __forceinline__ float group_sum(float v, int lanes) {
+    if (lanes >= 2) v = add_dpp<0xB1>(v);    // quad_perm 1,0,3,2
+    if (lanes >= 4) v = add_dpp<0x4E>(v);    // quad_perm 2,3,0,1
+    if (lanes >= 8) v = add_dpp<0x141>(v);   // row_half_mirror: quads of 8 lanes
+    if (lanes >= 16) v = add_dpp<0x140>(v);  // row_mirror: halves of 16 lanes
+    if (lanes >= 32) v += __shfl_xor(v, 16, 64);
+    if (lanes >= 64) v += __shfl_xor(v, 32, 64);
+    return v;
+}
+
+// Column sums of partial[rows][cols] in a fixed order: the gradients of parameters, which every workgroup adds to.  The
+// first `first` columns go to `out0`, the next `second` to out1, the rest to out2.  No rows: zeros.
+struct SumOut {
+    float *out0, *out1, *out2;
+    int64_t first, second;
+};
+constexpr int kSumThreads = 256, kSumCols = 32;
+namespace {
+__global__ __launch_bounds__(kSumThreads) void sum_partials(const float *__restrict__ partial, int64_t rows, int64_t cols, SumOut out) {
+    constexpr int kSlots = kSumThreads / kSumCols;
+    __shared__ float red[kSlots][kSumCols];
+    const int slot = threadIdx.x / kSumCols, c = threadIdx.x % kSumCols;
+    const int64_t col = (int64_t)blockIdx.x * kSumCols + c;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (col < cols) {
+        int64_t r = slot;
+        for (; r + 3 * kSlots < rows; r += 4 * kSlots)
+#pragma unroll
+            for (int i = 0; i < 4; i++) sum[i] += partial[(r + i * kSlots) * cols + col];
+        for (; r < rows; r += kSlots) sum[0] += partial[r * cols + col];
+    }
+    red[slot][c] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    __syncthreads();
+    if (slot == 0 && col < cols) {
+        float v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kSlots; i++) v += red[i][c];
+        float *const to = col < out.first ? out.out0 + col : col < out.first + out.second ? out.out1 + (col - out.first) : out.out2 + (col - out.first - out.second);
+        if ((col < out.first ? out.out0 : col < out.first + out.second ? out.out1 : out.out2) != nullptr) *to = v;
+    }
+}
+inline int launch_sum_partials(const float *partial, int64_t rows, int64_t cols, const SumOut &out, hipStream_t stream) {
+    sum_partials<<<dim3((unsigned)ceil_div(cols, kSumCols)), dim3(kSumThreads), 0, stream>>>(partial, rows, cols, out);
+    return check_launch("sum_partials");
+}
+}  // namespace
+
+}  // namespace ptq4vm

@@ -7,6 +7,7 @@
 // of entry points, which is filled once from the loaded libptq4vm.so.
 #include <ATen/ATen.h>
 #include <Python.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -28,7 +29,10 @@ struct Raised {};  // a Python exception is set
 #define PTQ4VM_HOT_ENTRIES(X)                                                                                      \
     X(quantize_pts) X(quantize_dynamic) X(quantize_pts_offset) X(quantize_pts_a4) X(quantize_pts_a4_e2m3)          \
     X(w8a8_linear) X(w8a8_linear_offset) X(w4a4_linear) X(w4a4_linear_e2m3) X(w8a8_linear_fused)                   \
-    X(w8a8_linear_offset_fused) X(w4a4_linear_fused) X(f16_linear)
+    X(w8a8_linear_offset_fused) X(w4a4_linear_fused) X(f16_linear)                                                 \
+    X(gated_scan) X(gated_scan_workspace) X(gated_scan_backward) X(gated_scan_backward_workspace) X(gated_scan_step) \
+    X(token_conv) X(token_conv_backward) X(token_conv_backward_workspace) X(token_conv_step) X(residual_norm)      \
+    X(residual_norm_backward) X(residual_norm_backward_workspace)
 
 struct Entries {
 #define X(name) decltype(&ptq4vm_##name) name = nullptr;
@@ -67,6 +71,7 @@ void launch(F &&f) {
 const char *dtype_name(at::ScalarType t) {
     switch (t) {
         case at::kHalf: return "torch.float16";
+        case at::kBFloat16: return "torch.bfloat16";
         case at::kChar: return "torch.int8";
         case at::kByte: return "torch.uint8";
         case at::kInt: return "torch.int32";
@@ -380,8 +385,311 @@ PyObject *f16_linear(Args a) {  // x w bias y
     return out.release();
 }
 
+// ---------------------------------------------------------------------------------- the operators between a block's linears
+// Their tensors have to be on one device, which need not be the current one: the call goes to that device's current stream.
+struct Operands {
+    at::ScalarType dtype;  // T of the first one
+    int code;              // its ptq4vm_dtype
+    at::Device device;
+
+    static const at::Tensor &first(PyObject *o, const char *name) {
+        const at::Tensor *t = tensor(o);
+        if (!t || !t->is_cuda() || (t->scalar_type() != at::kHalf && t->scalar_type() != at::kBFloat16 && t->scalar_type() != at::kFloat))
+            raise(PyExc_TypeError, std::string(name) + ": expected a 2-D CUDA tensor of torch.float16, torch.bfloat16 or torch.float32");
+        return *t;
+    }
+    static int code_of(at::ScalarType t) { return t == at::kHalf ? PTQ4VM_F16 : t == at::kBFloat16 ? PTQ4VM_BF16 : PTQ4VM_F32; }
+    Operands(PyObject *o, const char *name) : dtype(first(o, name).scalar_type()), code(code_of(dtype)), device(first(o, name).device()) {}
+
+    void here(PyObject *o, const char *name) const {
+        if (THPVariable_Unpack(o).device() != device) raise(PyExc_ValueError, std::string(name) + ": on another device than the first operand");
+    }
+    // [rows, cols] of T (or `type`)
+    Matrix in(PyObject *o, int64_t rows, int64_t cols, const char *name) const { return in(o, dtype, rows, cols, name); }
+    Matrix in(PyObject *o, at::ScalarType type, int64_t rows, int64_t cols, const char *name) const {
+        const Matrix m = matrix(o, type, name);
+        here(o, name);
+        if (m.rows != rows || m.cols != cols)
+            raise(PyExc_ValueError, std::string(name) + ": expected " + std::to_string(rows) + " x " + std::to_string(cols) + " elements, got " + std::to_string(m.rows) +
+                                        " x " + std::to_string(m.cols));
+        return m;
+    }
+    Matrix optional(PyObject *o, at::ScalarType type, int64_t rows, int64_t cols, const char *name) const {
+        return given(o) ? in(o, type, rows, cols, name) : Matrix{rows, cols, cols, nullptr};
+    }
+    Matrix out(PyObject *o, at::ScalarType type, int64_t rows, int64_t cols, const char *name) const {
+        const Matrix m = written(o, type, rows, cols, name);
+        here(o, name);
+        return m;
+    }
+    const float *floats(PyObject *o, int64_t n, const char *name, bool optional = false) const {
+        void *p = vector(o, at::kFloat, n, name, optional);
+        if (p || given(o)) here(o, name);
+        return static_cast<const float *>(p);
+    }
+    void *dense(PyObject *o, at::ScalarType type, at::IntArrayRef shape, const char *name) const {
+        const at::Tensor *t = tensor(o);
+        if (!t || !t->is_cuda() || t->scalar_type() != type || t->sizes() != shape || !t->is_contiguous()) {
+            std::string s;
+            for (const int64_t n : shape) s += (s.empty() ? "" : ", ") + std::to_string(n);
+            raise(PyExc_TypeError, std::string(name) + ": expected a contiguous CUDA tensor [" + s + "] of " + dtype_name(type));
+        }
+        here(o, name);
+        return t->data_ptr();
+    }
+    void *dense_or_null(PyObject *o, at::ScalarType type, at::IntArrayRef shape, const char *name) const {
+        return given(o) ? dense(o, type, shape, name) : nullptr;
+    }
+    at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const { return at::empty(shape, at::TensorOptions().dtype(type).device(device)); }
+    // Scratch of the call: the allocator gives it to nobody else before the work enqueued here is done
+    at::Tensor scratch(int64_t bytes) const { return bytes > 0 ? empty({bytes}, at::kByte) : at::Tensor(); }
+
+    template <typename F>
+    void launch(F &&f) const {
+        const c10::DeviceGuard guard(device);
+        ::launch(f);
+    }
+};
+
+bool truth(PyObject *o, bool otherwise) {
+    if (!o) return otherwise;
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised{};
+    return v != 0;
+}
+float real(PyObject *o, double otherwise) {
+    if (!o) return (float)otherwise;
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Raised{};
+    return (float)v;
+}
+void *scratch_data(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+int64_t scratch_bytes(const at::Tensor &t) { return t.defined() ? t.numel() : 0; }
+void not_the_same(const void *a, const void *b, const char *name) {
+    if (a && a == b) raise(PyExc_ValueError, std::string(name) + ": not the buffer of state");
+}
+
+PyObject *wrap(const at::Tensor &t) {
+    PyObject *o = THPVariable_Wrap(t);
+    if (!o) throw Raised{};
+    return o;
+}
+// The values as a tuple, None for a null pointer; the references stay with the callers' Owned
+template <size_t N>
+PyObject *tuple_of(PyObject *const (&items)[N]) {
+    PyObject *t = PyTuple_New(N);
+    if (!t) throw Raised{};
+    for (size_t i = 0; i < N; i++) {
+        PyObject *o = items[i] ? items[i] : Py_None;
+        Py_INCREF(o);
+        PyTuple_SET_ITEM(t, i, o);
+    }
+    return t;
+}
+
+struct ScanInputs {
+    Matrix u, dt, b, c, z;
+    const float *a, *d, *dt_bias;
+    int64_t K, N;
+    // u dt a b c d z dt_bias, from `at` on
+    ScanInputs(const Operands &ops, Args at) : u(matrix(at[0], ops.dtype, "u")) {
+        const int64_t M = u.rows;
+        K = u.cols;
+        ops.here(at[0], "u");
+        const at::Tensor *t = tensor(at[2]);
+        if (!t || t->dim() != 2) raise(PyExc_TypeError, "a: expected a contiguous CUDA tensor [K, N] of torch.float32");
+        N = t->size(1);
+        dt = ops.in(at[1], M, K, "dt");
+        a = static_cast<const float *>(ops.dense(at[2], at::kFloat, {K, N}, "a"));
+        b = ops.in(at[3], M, N, "b");
+        c = ops.in(at[4], M, N, "c");
+        d = ops.floats(at[5], K, "d", true);
+        z = ops.optional(at[6], ops.dtype, M, K, "z");
+        dt_bias = ops.floats(at[7], K, "dt_bias", true);
+    }
+};
+
+PyObject *gated_scan(Args a) {  // u dt a b c d z dt_bias B L reverse state y state_out marks
+    const Operands ops(a[0], "u");
+    const ScanInputs in(ops, a);
+    const int64_t B = integer(a[8]), L = integer(a[9]), K = in.K, N = in.N;
+    if (!is_product(in.u.rows, B, L)) raise(PyExc_ValueError, "u must have B*L rows");
+    const bool reverse = truth(a[10], false);
+    const float *state = floats(ops.dense_or_null(a[11], at::kFloat, {B, K, N}, "state"));
+    Owned out(output(a[12], {in.u.rows, K}, ops.dtype, a[0]));
+    const Matrix y = ops.out(out.o, ops.dtype, in.u.rows, K, "y");
+    float *const state_out = static_cast<float *>(ops.dense_or_null(a[13], at::kFloat, {B, K, N}, "state_out"));
+    not_the_same(state, state_out, "state_out");
+    float *const marks = given(a[14]) ? static_cast<float *>(ops.dense(a[14], at::kFloat, {PTQ4VM_SCAN_MARKS(L), B, K, N}, "marks")) : nullptr;
+    const at::Tensor ws = ops.scratch(entry.gated_scan_workspace(B, L, K, N));
+    ops.launch([&](void *s) { return entry.gated_scan(ops.code, in.u.data, in.dt.data, in.a, in.b.data, in.c.data, in.d, in.z.data, in.dt_bias, state, y.data, state_out,
+                               marks, scratch_data(ws), scratch_bytes(ws), reverse, B, L, K, N, in.u.ld, in.dt.ld, in.b.ld, in.c.ld, in.z.ld, y.ld, s); });
+    return out.release();
+}
+
+PyObject *gated_scan_backward(Args a) {  // dy u dt a b c d z dt_bias marks B L reverse du ddt db dc dz
+    const Operands ops(a[1], "u");
+    const ScanInputs in(ops, a + 1);
+    const int64_t B = integer(a[10]), L = integer(a[11]), M = in.u.rows, K = in.K, N = in.N;
+    if (!is_product(M, B, L)) raise(PyExc_ValueError, "u must have B*L rows");
+    const Matrix dy = ops.in(a[0], M, K, "dy");
+    if (L <= 0) raise(PyExc_ValueError, "L must be positive");
+    const float *marks = floats(ops.dense(a[9], at::kFloat, {PTQ4VM_SCAN_MARKS(L), B, K, N}, "marks"));
+    const bool reverse = truth(a[12], false);
+    if (given(a[17]) && !in.z.data && !given(a[7])) raise(PyExc_ValueError, "dz: there is no z");
+    Owned o_du(output(a[13], {M, K}, ops.dtype, a[1])), o_ddt(output(a[14], {M, K}, ops.dtype, a[1])), o_db(output(a[15], {M, N}, ops.dtype, a[1])),
+        o_dc(output(a[16], {M, N}, ops.dtype, a[1])), o_dz(given(a[7]) ? output(a[17], {M, K}, ops.dtype, a[1]) : nullptr);
+    const Matrix du = ops.out(o_du.o, ops.dtype, M, K, "du"), ddt = ops.out(o_ddt.o, ops.dtype, M, K, "ddt"), db = ops.out(o_db.o, ops.dtype, M, N, "db"),
+                 dc = ops.out(o_dc.o, ops.dtype, M, N, "dc"), dz = o_dz.o ? ops.out(o_dz.o, ops.dtype, M, K, "dz") : Matrix{M, K, K, nullptr};
+    const at::Tensor t_da = ops.empty({K, N}, at::kFloat), t_dd = given(a[6]) ? ops.empty({K}, at::kFloat) : at::Tensor(),
+                     t_bias = given(a[8]) ? ops.empty({K}, at::kFloat) : at::Tensor();
+    const at::Tensor ws = ops.scratch(entry.gated_scan_backward_workspace(B, L, K, N));
+    const auto data = [](const at::Tensor &t) { return t.defined() ? static_cast<float *>(t.data_ptr()) : nullptr; };
+    ops.launch([&](void *s) { return entry.gated_scan_backward(ops.code, dy.data, in.u.data, in.dt.data, in.a, in.b.data, in.c.data, in.d, in.z.data, in.dt_bias, marks, du.data,
+                               ddt.data, data(t_da), db.data, dc.data, data(t_dd), dz.data, data(t_bias), scratch_data(ws), scratch_bytes(ws), reverse, B, L, K, N, dy.ld,
+                               in.u.ld, in.dt.ld, in.b.ld, in.c.ld, in.z.ld, du.ld, ddt.ld, db.ld, dc.ld, dz.ld, s); });
+    Owned da(wrap(t_da)), dd(t_dd.defined() ? wrap(t_dd) : nullptr), dbias(t_bias.defined() ? wrap(t_bias) : nullptr);
+    return tuple_of({o_du.o, o_ddt.o, da.o, o_db.o, o_dc.o, dd.o, o_dz.o, dbias.o});
+}
+
+PyObject *gated_scan_step(Args a) {  // u dt a b c d z dt_bias state y state_out
+    const Operands ops(a[0], "u");
+    const ScanInputs in(ops, a);
+    const int64_t B = in.u.rows, K = in.K, N = in.N;
+    float *const state = static_cast<float *>(ops.dense(a[8], at::kFloat, {B, K, N}, "state"));
+    Owned out(output(a[9], {B, K}, ops.dtype, a[0]));
+    const Matrix y = ops.out(out.o, ops.dtype, B, K, "y");
+    float *const state_out = given(a[10]) ? static_cast<float *>(ops.dense(a[10], at::kFloat, {B, K, N}, "state_out")) : state;
+    ops.launch([&](void *s) { return entry.gated_scan_step(ops.code, in.u.data, in.dt.data, in.a, in.b.data, in.c.data, in.d, in.z.data, in.dt_bias, state, y.data, state_out, B,
+                               K, N, in.u.ld, in.dt.ld, in.b.ld, in.c.ld, in.z.ld, y.ld, s); });
+    return out.release();
+}
+
+struct ConvInputs {
+    Matrix x;
+    const float *w, *bias;
+    int64_t K, W;
+    ConvInputs(const Operands &ops, Args at) : x(matrix(at[0], ops.dtype, "x")) {  // x w bias, from `at` on
+        K = x.cols;
+        const at::Tensor *t = tensor(at[1]);
+        if (!t || t->dim() != 2 || t->size(1) < 2 || t->size(1) > 4) raise(PyExc_TypeError, "w: expected a contiguous CUDA tensor [K, 2..4] of torch.float32");
+        W = t->size(1);
+        w = floats(ops.dense(at[1], at::kFloat, {K, W}, "w"));
+        bias = ops.floats(at[2], K, "bias", true);
+    }
+};
+
+PyObject *token_conv(Args a) {  // x w bias B L silu reverse state y state_out
+    const Operands ops(a[0], "x");
+    const ConvInputs in(ops, a);
+    const int64_t B = integer(a[3]), L = integer(a[4]), K = in.K, W = in.W;
+    same_rows(in.x.rows, B, L);
+    const bool silu = truth(a[5], true), reverse = truth(a[6], false);
+    const void *state = ops.dense_or_null(a[7], ops.dtype, {B, W - 1, K}, "state");
+    Owned out(output(a[8], {in.x.rows, K}, ops.dtype, a[0]));
+    const Matrix y = ops.out(out.o, ops.dtype, in.x.rows, K, "y");
+    void *const state_out = ops.dense_or_null(a[9], ops.dtype, {B, W - 1, K}, "state_out");
+    not_the_same(state, state_out, "state_out");
+    ops.launch([&](void *s) { return entry.token_conv(ops.code, in.x.data, in.w, in.bias, state, y.data, state_out, silu, reverse, B, L, K, W, in.x.ld, y.ld, s); });
+    return out.release();
+}
+
+PyObject *token_conv_backward(Args a) {  // dy x w bias B L silu reverse state dx
+    const Operands ops(a[1], "x");
+    const ConvInputs in(ops, a + 1);
+    const int64_t B = integer(a[4]), L = integer(a[5]), M = in.x.rows, K = in.K, W = in.W;
+    same_rows(M, B, L);
+    const Matrix dy = ops.in(a[0], M, K, "dy");
+    const bool silu = truth(a[6], true), reverse = truth(a[7], false);
+    const void *state = ops.dense_or_null(a[8], ops.dtype, {B, W - 1, K}, "state");
+    Owned o_dx(output(a[9], {M, K}, ops.dtype, a[1]));
+    const Matrix dx = ops.out(o_dx.o, ops.dtype, M, K, "dx");
+    const at::Tensor t_dw = ops.empty({K, W}, at::kFloat), t_db = given(a[3]) ? ops.empty({K}, at::kFloat) : at::Tensor();
+    const at::Tensor ws = ops.scratch(entry.token_conv_backward_workspace(B, L, K, W));
+    float *const dbias = t_db.defined() ? static_cast<float *>(t_db.data_ptr()) : nullptr;
+    ops.launch([&](void *s) { return entry.token_conv_backward(ops.code, dy.data, in.x.data, in.w, in.bias, state, dx.data, static_cast<float *>(t_dw.data_ptr()), dbias,
+                               scratch_data(ws), scratch_bytes(ws), silu, reverse, B, L, K, W, dy.ld, in.x.ld, dx.ld, s); });
+    Owned o_dw(wrap(t_dw)), o_db(t_db.defined() ? wrap(t_db) : nullptr);
+    return tuple_of({o_dx.o, o_dw.o, o_db.o});
+}
+
+PyObject *token_conv_step(Args a) {  // x w bias state silu y state_out
+    const Operands ops(a[0], "x");
+    const ConvInputs in(ops, a);
+    const int64_t B = in.x.rows, K = in.K, W = in.W;
+    void *const state = ops.dense(a[3], ops.dtype, {B, W - 1, K}, "state");
+    const bool silu = truth(a[4], true);
+    Owned out(output(a[5], {B, K}, ops.dtype, a[0]));
+    const Matrix y = ops.out(out.o, ops.dtype, B, K, "y");
+    void *const state_out = given(a[6]) ? ops.dense(a[6], ops.dtype, {B, W - 1, K}, "state_out") : state;
+    ops.launch([&](void *s) { return entry.token_conv_step(ops.code, in.x.data, in.w, in.bias, state, y.data, state_out, silu, B, K, W, in.x.ld, y.ld, s); });
+    return out.release();
+}
+
+// The residual stream's type: that of the first of these that is given
+at::ScalarType stream_type(const Operands &ops, PyObject *o, PyObject *other, const char *name) {
+    const at::Tensor *t = given(o) ? tensor(o) : given(other) ? tensor(other) : nullptr;
+    if (!given(o) && !given(other)) return ops.dtype;
+    if (!t || (t->scalar_type() != ops.dtype && t->scalar_type() != at::kFloat))
+        raise(PyExc_TypeError, std::string(name) + ": expected a 2-D CUDA tensor of " + dtype_name(ops.dtype) + " or torch.float32");
+    return t->scalar_type();
+}
+struct Gate {
+    const float *data = nullptr;
+    int64_t rows = 0;
+    Gate(const Operands &ops, PyObject *o, int64_t M, int64_t K) {
+        if (!given(o)) return;
+        const at::Tensor *t = tensor(o);
+        if (!t || t->dim() != 2) raise(PyExc_TypeError, "gate: expected a contiguous CUDA tensor [G, K] of torch.float32");
+        rows = t->size(0);
+        data = floats(ops.dense(o, at::kFloat, {rows, K}, "gate"));
+        if (rows <= 0 || M % rows != 0) raise(PyExc_ValueError, "gate: its rows must divide those of h");
+    }
+};
+
+PyObject *residual_norm(Args a) {  // h residual w gate w_post scale eps y residual_out
+    const Operands ops(a[0], "h");
+    const Matrix h = matrix(a[0], ops.dtype, "h");
+    const int64_t M = h.rows, K = h.cols;
+    const at::ScalarType type = stream_type(ops, a[1], a[8], given(a[1]) ? "residual" : "residual_out");
+    const Matrix residual = ops.optional(a[1], type, M, K, "residual");
+    const float *w = ops.floats(a[2], K, "w"), *w_post = ops.floats(a[4], K, "w_post", true);
+    const Gate gate(ops, a[3], M, K);
+    const float scale = real(a[5], 1.0), eps = real(a[6], 1e-5);
+    Owned o_y(output(a[7], {M, K}, ops.dtype, a[0])), o_r(output(a[8], {M, K}, type, a[0]));
+    const Matrix y = ops.out(o_y.o, ops.dtype, M, K, "y"), r = ops.out(o_r.o, type, M, K, "residual_out");
+    ops.launch([&](void *s) { return entry.residual_norm(ops.code, Operands::code_of(type), h.data, residual.data, w, gate.data, w_post, y.data, r.data, scale, eps, M, K, gate.rows,
+                               h.ld, residual.ld, y.ld, r.ld, s); });
+    return tuple_of({o_y.o, o_r.o});
+}
+
+PyObject *residual_norm_backward(Args a) {  // dy dr h r w gate w_post scale eps first dh dresidual
+    const Operands ops(a[2], "h");
+    const Matrix h = matrix(a[2], ops.dtype, "h");
+    const int64_t M = h.rows, K = h.cols;
+    const Matrix dy = ops.in(a[0], M, K, "dy");
+    const at::ScalarType type = stream_type(ops, a[3], nullptr, "r");
+    const Matrix r = ops.in(a[3], type, M, K, "r"), dr = ops.optional(a[1], type, M, K, "dr");
+    const float *w = ops.floats(a[4], K, "w"), *w_post = ops.floats(a[6], K, "w_post", true);
+    const Gate gate(ops, a[5], M, K);
+    const float scale = real(a[7], 1.0), eps = real(a[8], 1e-5);
+    const bool first = truth(a[9], false);
+    if (first && given(a[11])) raise(PyExc_ValueError, "dresidual: there is no residual");
+    Owned o_dh(output(a[10], {M, K}, ops.dtype, a[2])), o_dres(first ? nullptr : output(a[11], {M, K}, type, a[2]));
+    const Matrix dh = ops.out(o_dh.o, ops.dtype, M, K, "dh"), dres = first ? Matrix{M, K, K, nullptr} : ops.out(o_dres.o, type, M, K, "dresidual");
+    const at::Tensor t_dw = ops.empty({K}, at::kFloat), t_dgate = gate.data || given(a[5]) ? ops.empty({gate.rows, K}, at::kFloat) : at::Tensor(),
+                     t_dpost = w_post ? ops.empty({K}, at::kFloat) : at::Tensor();
+    const at::Tensor ws = ops.scratch(entry.residual_norm_backward_workspace(M, K, gate.rows));
+    const auto data = [](const at::Tensor &t) { return t.defined() ? static_cast<float *>(t.data_ptr()) : nullptr; };
+    ops.launch([&](void *s) { return entry.residual_norm_backward(ops.code, Operands::code_of(type), dy.data, dr.data, h.data, r.data, w, gate.data, w_post, dh.data, dres.data,
+                               data(t_dw), data(t_dgate), data(t_dpost), scratch_data(ws), scratch_bytes(ws), scale, eps, M, K, gate.rows, dy.ld, dr.ld, h.ld, r.ld, dh.ld,
+                               dres.ld, s); });
+    Owned dw(wrap(t_dw)), dgate(t_dgate.defined() ? wrap(t_dgate) : nullptr), dpost(t_dpost.defined() ? wrap(t_dpost) : nullptr);
+    return tuple_of({o_dh.o, o_dres.o, dw.o, dgate.o, dpost.o});
+}
+
 // ---------------------------------------------------------------------------------- Python signatures
-constexpr int kMaxParams = 13;
+constexpr int kMaxParams = 18;
 
 struct Signature {
     const char *function;
@@ -454,6 +762,14 @@ SIG(w8a8_linear_fused, 8, 11, "x", "inv_m", "s_tok", "wq", "s_w", "bias", "B", "
 SIG(w8a8_linear_offset_fused, 10, 13, "x", "inv_m", "s_tok", "z_tok", "wq", "rowsum", "s_w", "bias", "B", "L", "y", "acc_out", "xq_out")
 SIG(w4a4_linear_fused, 8, 11, "x", "inv_m", "s_tok", "wq4", "s_w", "bias", "B", "L", "y", "acc_out", "xq_out")
 SIG(f16_linear, 3, 4, "x", "w", "bias", "y")
+SIG(gated_scan, 10, 15, "u", "dt", "a", "b", "c", "d", "z", "dt_bias", "B", "L", "reverse", "state", "y", "state_out", "marks")
+SIG(gated_scan_backward, 12, 18, "dy", "u", "dt", "a", "b", "c", "d", "z", "dt_bias", "marks", "B", "L", "reverse", "du", "ddt", "db", "dc", "dz")
+SIG(gated_scan_step, 9, 11, "u", "dt", "a", "b", "c", "d", "z", "dt_bias", "state", "y", "state_out")
+SIG(token_conv, 5, 10, "x", "w", "bias", "B", "L", "silu", "reverse", "state", "y", "state_out")
+SIG(token_conv_backward, 6, 10, "dy", "x", "w", "bias", "B", "L", "silu", "reverse", "state", "dx")
+SIG(token_conv_step, 4, 7, "x", "w", "bias", "state", "silu", "y", "state_out")
+SIG(residual_norm, 3, 9, "h", "residual", "w", "gate", "w_post", "scale", "eps", "y", "residual_out")
+SIG(residual_norm_backward, 5, 12, "dy", "dr", "h", "r", "w", "gate", "w_post", "scale", "eps", "first", "dh", "dresidual")
 #undef SIG
 
 // bind({name: address of ptq4vm_<name>}): the entry points of the loaded library
@@ -511,6 +827,24 @@ PyMethodDef methods[] = {
                             "ptq4vm_w4a4_linear_fused: y fp16 [B*L, N] from fp16 activations and a packed 4-bit weight [N, K/2];\n"
                             "acc_out / xq_out (int8, one 4-bit code per byte) are filled if given."),
     FAST(f16_linear, "f16_linear(x, w, bias, y=None)\n--\n\nptq4vm_f16_linear: y fp16 [M, N]."),
+    FAST(gated_scan, "gated_scan(u, dt, a, b, c, d, z, dt_bias, B, L, reverse=False, state=None, y=None, state_out=None, marks=None)\n--\n\n"
+                     "ptq4vm_gated_scan: y [B*L, K] of u's type (fp16, bfloat16, fp32); state_out (f32 [B, K, N], not state itself) and marks\n"
+                     "(f32 [scan_marks(L), B, K, N], for the backward pass) are filled if given."),
+    FAST(gated_scan_backward, "gated_scan_backward(dy, u, dt, a, b, c, d, z, dt_bias, marks, B, L, reverse=False, du=None, ddt=None, db=None, dc=None, dz=None)\n--\n\n"
+                              "ptq4vm_gated_scan_backward: (du, ddt, da, db, dc, dd, dz, ddt_bias); None for the gradient of an input that is None."),
+    FAST(gated_scan_step, "gated_scan_step(u, dt, a, b, c, d, z, dt_bias, state, y=None, state_out=None)\n--\n\n"
+                          "ptq4vm_gated_scan_step: y [B, K] for one token of each sequence; state (f32 [B, K, N]) advances in place unless state_out is given."),
+    FAST(token_conv, "token_conv(x, w, bias, B, L, silu=True, reverse=False, state=None, y=None, state_out=None)\n--\n\n"
+                     "ptq4vm_token_conv: y [B*L, K] of x's type; state_out ([B, W - 1, K] of x's type, not state itself) is filled if given."),
+    FAST(token_conv_backward, "token_conv_backward(dy, x, w, bias, B, L, silu=True, reverse=False, state=None, dx=None)\n--\n\n"
+                              "ptq4vm_token_conv_backward: (dx, dw, dbias); dbias is None without a bias."),
+    FAST(token_conv_step, "token_conv_step(x, w, bias, state, silu=True, y=None, state_out=None)\n--\n\n"
+                          "ptq4vm_token_conv_step: y [B, K] for one token of each sequence; state ([B, W - 1, K]) advances in place unless state_out is given."),
+    FAST(residual_norm, "residual_norm(h, residual, w, gate=None, w_post=None, scale=1.0, eps=1e-5, y=None, residual_out=None)\n--\n\n"
+                        "ptq4vm_residual_norm: (y, residual_out); residual_out has residual's type, h's where residual is None and none is given."),
+    FAST(residual_norm_backward, "residual_norm_backward(dy, dr, h, r, w, gate=None, w_post=None, scale=1.0, eps=1e-5, first=False, dh=None, dresidual=None)\n--\n\n"
+                                 "ptq4vm_residual_norm_backward, r the forward pass's residual_out and dr its gradient or None: (dh, dresidual, dw, dgate,\n"
+                                 "dw_post); dresidual is None with first=True (no residual), dgate and dw_post without gate and w_post."),
     {"bind", bind, METH_O, "bind(table)\n--\n\nAddresses of the library's entry points by name, without the ptq4vm_ prefix."},
     {"setup", setup, METH_VARARGS, "setup(load_library, raise_status)\n--\n\nCallbacks: load the library and bind(); raise for a status."},
     {nullptr, nullptr, 0, nullptr}};
@@ -522,7 +856,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "Launches of libptq4vm.so
 PyMODINIT_FUNC PyInit__calls() {
     for (Signature *s : {&sig_quantize_pts, &sig_quantize_dynamic, &sig_quantize_pts_offset, &sig_quantize_pts_a4, &sig_quantize_pts_a4_e2m3,
                          &sig_w8a8_linear, &sig_w8a8_linear_offset, &sig_w4a4_linear, &sig_w4a4_linear_e2m3, &sig_w8a8_linear_fused,
-                         &sig_w8a8_linear_offset_fused, &sig_w4a4_linear_fused, &sig_f16_linear})
+                         &sig_w8a8_linear_offset_fused, &sig_w4a4_linear_fused, &sig_f16_linear, &sig_gated_scan, &sig_gated_scan_backward,
+                         &sig_gated_scan_step, &sig_token_conv, &sig_token_conv_backward, &sig_token_conv_step, &sig_residual_norm, &sig_residual_norm_backward})
         for (int i = 0; i < s->total; i++) s->interned[i] = PyUnicode_InternFromString(s->names[i]);
     return PyModule_Create(&module);
 }
