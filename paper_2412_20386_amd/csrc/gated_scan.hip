@@ -5,16 +5,18 @@ namespace {
 
 using namespace ptq4vm;
 
+constexpr int kAhead = 8;  // chunks whose states are loaded together
+
 // One wavefront: 16 C channels of one sequence through the tokens of one chunk.
 // STATES_ONLY: from a zero state, without outputs; leaves the chunk's end state and its sum of D, from which the chunks behind
 // it know their first state: h_in(i + 1) = exp(a sum D(i)) h_in(i) + h_end(i).
-// PADDED: N is no multiple of what a quad holds; the states behind N are kept at zero.
-template <typename T, int NS, int C, bool PADDED, bool STATES_ONLY>
-__global__ __launch_bounds__(64) void gated_scan_tokens(ScanArgs<T> p) {
+// RAGGED: K or N leave lanes without a channel or a state; the states behind N are kept at zero.
+template <typename T, int NS, int C, bool RAGGED, bool STATES_ONLY>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 2 : 4))) void gated_scan_tokens(ScanArgs<T> p) {
     using S = ScanLane<NS, C>;
-    __shared__ float2 steps[kTile][S::kChannels];  // D and D u
-    __shared__ float sums[kTile][S::kChannels];    // s without its d u
-    __shared__ float sb[kTile][S::kStates], sc[kTile][S::kStates];
+    alignas(16) __shared__ float2 steps[kTile][S::kChannels];  // D and D u
+    alignas(16) __shared__ float sums[kTile][S::kChannels];    // s without its d u
+    alignas(16) __shared__ float sb[kTile][S::kStates], sc[kTile][S::kStates];
     const uint32_t block = xcd_contiguous(blockIdx.x, p.blocks);
     if (block >= p.blocks) return;
     const int cb = block % p.column_blocks, bc = block / p.column_blocks, b = bc % p.B;
@@ -23,72 +25,73 @@ __global__ __launch_bounds__(64) void gated_scan_tokens(ScanArgs<T> p) {
     const int64_t t_begin = chunk * p.chunk_tokens, t_end = min(p.L, t_begin + p.chunk_tokens);
 
     float a2[C][NS], h[C][NS], sum_d[C];
+    const int kc = cb * S::kChannels + cl * C;  // the quad's first channel
 #pragma unroll
     for (int c = 0; c < C; c++) {
-        const int k = cb * S::kChannels + cl * C + c, n = k < p.K ? p.N : 0;
-        const int64_t at = ((int64_t)b * p.K + k) * p.N;
-        load_channel<NS>(p.a + (int64_t)(k < p.K ? k : 0) * p.N, n0, n, a2[c]);
+        const bool mine = !RAGGED || kc + c < p.K;
+        load_channel<NS, RAGGED>(p.a, kc + c, n0, p.N, mine, a2[c]);
         sum_d[c] = 0.0f;
 #pragma unroll
         for (int i = 0; i < NS; i++) a2[c][i] *= kLog2e, h[c][i] = 0.0f;
         if constexpr (!STATES_ONLY) {
-            if (p.state) load_channel<NS>(p.state + (n ? at : 0), n0, n, h[c]);
-            for (uint32_t i = 0; i < chunk; i++) {
-                const int64_t from = (int64_t)i * p.B * p.K;
-                float end[NS];
-                load_channel<NS>(p.chunk_state + (n ? from * p.N + at : 0), n0, n, end);
-                const float D = n ? p.chunk_dt[from + (int64_t)b * p.K + k] : 0.0f;
+            if (p.state) load_channel<NS, RAGGED>(p.state, (int64_t)b * p.K + kc + c, n0, p.N, mine, h[c]);
+            for (uint32_t i = 0; i < chunk; i += kAhead) {  // (the loads of kAhead chunks are in flight together)
+                float end[kAhead][NS], D[kAhead];
 #pragma unroll
-                for (int j = 0; j < NS; j++) h[c][j] = fmaf(__builtin_amdgcn_exp2f(a2[c][j] * D), h[c][j], end[j]);
+                for (int s = 0; s < kAhead; s++) {
+                    const int64_t channel = ((int64_t)min(i + s, chunk - 1) * p.B + b) * p.K + (mine ? kc + c : 0);
+                    load_channel<NS, RAGGED>(p.chunk_state, channel, n0, p.N, mine, end[s]);
+                    D[s] = p.chunk_dt[channel];
+                }
+#pragma unroll
+                for (int s = 0; s < kAhead; s++)
+                    if (i + s < chunk)
+#pragma unroll
+                        for (int j = 0; j < NS; j++) h[c][j] = fmaf(__builtin_amdgcn_exp2f(a2[c][j] * D[s]), h[c][j], end[s][j]);
             }
         }
     }
 
     // what this lane loads: kVec channels of a token
     const int vt = lane / S::kAcross, vk = (lane % S::kAcross) * S::kVec, k = cb * S::kChannels + vk, nk = max(0, min(S::kVec, p.K - k));
-    float bias[S::kVec], skip[S::kVec];
-#pragma unroll
-    for (int i = 0; i < S::kVec; i++) {
-        bias[i] = p.dt_bias && i < nk ? p.dt_bias[k + i] : 0.0f;
-        skip[i] = !STATES_ONLY && p.d && i < nk ? p.d[k + i] : 0.0f;
+    alignas(16) __shared__ float bias[S::kChannels], skip[S::kChannels];
+    if (lane < S::kChannels) {
+        const int at = cb * S::kChannels + lane;
+        bias[lane] = p.dt_bias && at < p.K ? p.dt_bias[at] : 0.0f;
+        skip[lane] = p.d && at < p.K ? p.d[at] : 0.0f;
     }
-    T ru[S::kPasses][S::kVec], rdt[S::kPasses][S::kVec], rz[S::kPasses][S::kVec], rb[NS], rc[NS];
+    __syncthreads();
+    T ru[S::kVec], rdt[S::kVec], rz[S::kVec], rb[NS], rc[NS];
     const auto fetch = [&](int64_t t0) {
-#pragma unroll
-        for (int s = 0; s < S::kPasses; s++) {
-            const int64_t t = t0 + s * S::kTokens + vt;
-            const int n = t < t_end ? nk : 0;
-            load_first<S::kVec>(p.u.at(b, n ? t : 0) + k, n, ru[s]);
-            load_first<S::kVec>(p.dt.at(b, n ? t : 0) + k, n, rdt[s]);
-            if (!STATES_ONLY && p.z.data) load_first<S::kVec>(p.z.at(b, n ? t : 0) + k, n, rz[s]);
-        }
-        load_states<NS>(p.b, b, t0, t_end, p.N, rb);
-        if constexpr (!STATES_ONLY) load_states<NS>(p.c, b, t0, t_end, p.N, rc);
+        const int last = (int)min((int64_t)kTile, t_end - t0) - 1;
+        load_token<S::kVec, RAGGED>(p.u, b, t0, vt, last, k, nk, ru);
+        load_token<S::kVec, RAGGED>(p.dt, b, t0, vt, last, k, nk, rdt);
+        if (!STATES_ONLY && p.z.data) load_token<S::kVec, RAGGED>(p.z, b, t0, vt, last, k, nk, rz);
+        load_states<NS, RAGGED>(p.b, b, t0, last, p.N, rb);
+        if constexpr (!STATES_ONLY) load_states<NS, RAGGED>(p.c, b, t0, last, p.N, rc);
     };
     fetch(t_begin);
     for (int64_t t0 = t_begin; t0 < t_end; t0 += kTile) {
-        T u[S::kPasses][S::kVec], z[S::kPasses][S::kVec];
+        T u[S::kVec], z[S::kVec];
+        const bool there = t0 + vt < t_end;  // (tokens behind the last change nothing: D = 0)
 #pragma unroll
-        for (int s = 0; s < S::kPasses; s++) {
-            const bool there = t0 + s * S::kTokens + vt < t_end;  // (tokens behind the last change nothing: D = 0)
-#pragma unroll
-            for (int i = 0; i < S::kVec; i++) {
-                u[s][i] = ru[s][i];
-                if (!STATES_ONLY) z[s][i] = rz[s][i];
-                const float D = there ? softplus_of((float)rdt[s][i] + bias[i]) : 0.0f;
-                steps[s * S::kTokens + vt][vk + i] = {D, there ? D * (float)ru[s][i] : 0.0f};
-            }
+        for (int i = 0; i < S::kVec; i++) {
+            u[i] = ru[i];
+            if (!STATES_ONLY) z[i] = rz[i];
+            const float D = softplus_of((float)rdt[i] + bias[vk + i]);
+            steps[vt][vk + i] = {D, D * (float)ru[i]};
         }
+        if (!there)
+#pragma unroll
+            for (int i = 0; i < S::kVec; i++) steps[vt][vk + i] = {0.0f, 0.0f};
         keep_states<NS>(rb, sb);
         if constexpr (!STATES_ONLY) keep_states<NS>(rc, sc);
         __syncthreads();
         if (t0 + kTile < t_end) fetch(t0 + kTile);  // in flight under this tile's steps
         if (!STATES_ONLY && p.marks)
 #pragma unroll
-            for (int c = 0; c < C; c++) {
-                const int kc = cb * S::kChannels + cl * C + c;
-                if (kc < p.K) store_channel<NS>(p.marks + (((t0 / kTile) * p.B + b) * p.K + kc) * p.N, n0, p.N, h[c]);
-            }
+            for (int c = 0; c < C; c++)
+                store_channel<NS, RAGGED>(p.marks, ((t0 / kTile) * p.B + b) * p.K + kc + c, n0, p.N, kc + c < p.K, h[c]);
         const int groups = (int)((min((int64_t)kTile, t_end - t0) + 3) / 4);
         for (int g = 0; g < groups; g++)
 #pragma unroll
@@ -108,35 +111,29 @@ __global__ __launch_bounds__(64) void gated_scan_tokens(ScanArgs<T> p) {
 #pragma unroll
                     for (int i = 0; i < NS; i++) {
                         h[c][i] = fmaf(__builtin_amdgcn_exp2f(a2[c][i] * D.x), h[c][i], D.y * B[i]);
-                        if (PADDED) h[c][i] = n0 + i < p.N ? h[c][i] : 0.0f;
+                        if (RAGGED) h[c][i] = n0 + i < p.N ? h[c][i] : 0.0f;
                         if (!STATES_ONLY) v[c] = fmaf(h[c][i], CC[i], v[c]);
                     }
-                    if (!STATES_ONLY) v[c] = quad_sum(v[c]);
                 }
-                if constexpr (!STATES_ONLY)
-                    if (q < C) sums[t][cl * C + q] = C == 2 && q == 1 ? v[C - 1] : v[0];
+                if constexpr (!STATES_ONLY) sums[t][cl * C + q % C] = quad_sums<C>(v, q);  // (lanes of the same place write the same value)
             }
         __syncthreads();
-        if constexpr (!STATES_ONLY)
+        if constexpr (!STATES_ONLY) {
+            float y[S::kVec];
 #pragma unroll
-            for (int s = 0; s < S::kPasses; s++) {
-                const int64_t t = t0 + s * S::kTokens + vt;
-                float y[S::kVec];
+            for (int i = 0; i < S::kVec; i++) y[i] = fmaf(skip[vk + i], (float)u[i], sums[vt][vk + i]);
+            if (p.z.data)
 #pragma unroll
-                for (int i = 0; i < S::kVec; i++) {
-                    y[i] = fmaf(skip[i], (float)u[s][i], sums[s * S::kTokens + vt][vk + i]);
-                    if (p.z.data) y[i] *= (float)z[s][i] * sigmoid_of((float)z[s][i]);
-                }
-                if (t < t_end && nk) store_first<S::kVec>(p.y.at(b, t) + k, nk, y);
-            }
+                for (int i = 0; i < S::kVec; i++) y[i] *= (float)z[i] * sigmoid_of((float)z[i]);
+            if (there) store_token<S::kVec, RAGGED>(p.y, b, t0, vt, k, nk, y);
+        }
     }
     float *const out = STATES_ONLY ? p.chunk_state + (int64_t)chunk * p.B * p.K * p.N : t_end == p.L ? p.state_out : nullptr;
     if (out)
 #pragma unroll
         for (int c = 0; c < C; c++) {
-            const int kc = cb * S::kChannels + cl * C + c;
-            if (kc < p.K) store_channel<NS>(out + ((int64_t)b * p.K + kc) * p.N, n0, p.N, h[c]);
-            if (STATES_ONLY && kc < p.K && q == 0) p.chunk_dt[((int64_t)chunk * p.B + b) * p.K + kc] = sum_d[c];
+            store_channel<NS, RAGGED>(out, (int64_t)b * p.K + kc + c, n0, p.N, kc + c < p.K, h[c]);
+            if (STATES_ONLY && q == 0 && kc + c < p.K) p.chunk_dt[((int64_t)chunk * p.B + b) * p.K + kc + c] = sum_d[c];
         }
 }
 
@@ -153,8 +150,8 @@ __global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
     float h[NS], a[NS];
     T B[NS], CC[NS];
     const int n = max(0, min(NS, p.N - n0));
-    load_channel<NS>(p.state + ch * p.N, n0, p.N, h);
-    load_channel<NS>(p.a + (int64_t)k * p.N, n0, p.N, a);
+    load_channel<NS, true>(p.state, ch, n0, p.N, true, h);
+    load_channel<NS, true>(p.a, k, n0, p.N, true, a);
     load_first<NS>(p.b.at(b, 0) + n0, n, B);
     load_first<NS>(p.c.at(b, 0) + n0, n, CC);
     const float u = (float)p.u.at(b, 0)[k];
@@ -167,7 +164,7 @@ __global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
     }
     v = quad_sum(v);
     if (!there) return;
-    store_channel<NS>(p.state_out + ch * p.N, n0, p.N, h);
+    store_channel<NS, true>(p.state_out, ch, n0, p.N, true, h);
     if (q != 0) return;
     if (p.d) v = fmaf(p.d[k], u, v);
     if (p.z.data) {
@@ -183,6 +180,8 @@ int check_scan(int dtype, const void *u, const void *dt, const float *a, const v
     if (!a || (B != 0 && (!u || !dt || !b || !c || !y))) return PTQ4VM_ERR_NULL;  // (a matrix of no rows has no address)
     if (!scan_sizes(B, L, K, N)) return PTQ4VM_ERR_SHAPE;
     if (ldu < K || lddt < K || ldb < N || ldc < N || (z && ldz < K) || ldy < K) return PTQ4VM_ERR_STRIDE;
+    for (const int64_t ld : {ldu, lddt, ldb, ldc, z ? ldz : 0, ldy})
+        if (ld >= kMaxPitch) return PTQ4VM_ERR_STRIDE;
     const uintptr_t e = dtype_bytes(dtype);
     if (!aligned_to(u, e) || !aligned_to(dt, e) || !aligned_to(b, e) || !aligned_to(c, e) || !aligned_to(z, e) || !aligned_to(y, e) || !aligned_to(a, 4) ||
         !aligned_to(d, 4) || !aligned_to(dt_bias, 4))
@@ -228,10 +227,10 @@ int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, 
         s.state = state, s.state_out = state_out, s.marks = marks;
         s.chunk_state = static_cast<float *>(workspace), s.chunk_dt = s.chunk_state + (plan.chunks > 1 ? plan.chunks * B * K * N : 0);
         s.column_blocks = (int)plan.column_blocks, s.chunk_tokens = plan.chunk_tokens;
-        return for_layout(plan, N, [&](auto ns, auto ch, auto padded) {
+        return for_layout(plan, K, N, [&](auto ns, auto ch, auto ragged) {
             const auto go = [&](auto states_only, int64_t chunks) {
                 s.chunks = (uint32_t)chunks, s.blocks = (uint32_t)(chunks * B * plan.column_blocks);
-                gated_scan_tokens<T, ns(), ch(), padded(), states_only()><<<dim3(xcd_grid(s.blocks)), dim3(64), 0, stream>>>(s);
+                gated_scan_tokens<T, ns(), ch(), ragged(), states_only()><<<dim3(xcd_grid(s.blocks)), dim3(64), 0, stream>>>(s);
                 return check_launch("gated_scan_tokens");
             };
             if (plan.chunks > 1)  // (nobody asks for the last chunk's)

@@ -37,8 +37,7 @@ struct ScanLane {
     static constexpr int kStates = 4 * NS;               // that a quad has room for
     static constexpr int kVec = C == 1 ? 4 : 8;          // channels that a lane loads of one token
     static constexpr int kAcross = kChannels / kVec;     // lanes side by side
-    static constexpr int kTokens = 64 / kAcross;         // tokens that a wavefront loads at once
-    static constexpr int kPasses = kTile / kTokens;
+    static_assert(64 / kAcross == kTile, "the lanes of a wavefront load a tile at once");
 };
 
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -57,19 +56,20 @@ inline ScanPlan scan_plan(int64_t B, int64_t L, int64_t K, int64_t N) {
     ScanPlan p{channels_per_lane(B, K, N), states_per_lane(N), 0, 0, 0};
     p.column_blocks = ceil_div(K, 16 * p.channels);
     const int64_t waves = B * p.column_blocks;
-    int64_t chunks = waves >= 1024 ? 1 : ceil_div(2048, waves > 0 ? waves : 1);
+    int64_t chunks = waves >= 1024 ? 1 : ceil_div(4096, waves > 0 ? waves : 1);
     if (chunks > ceil_div(L, 2 * kTile)) chunks = ceil_div(L, 2 * kTile);
-    if (chunks > 64) chunks = 64;
+    if (chunks > 128) chunks = 128;
     p.chunk_tokens = ceil_div(ceil_div(L, chunks), kTile) * kTile;
     p.chunks = ceil_div(L, p.chunk_tokens);
     return p;
 }
 
+// f(NS, C, RAGGED): ragged where a wavefront's channels or a quad's states are not all there
 template <typename F>
-int for_layout(const ScanPlan &p, int64_t N, F &&f) {
+int for_layout(const ScanPlan &p, int64_t K, int64_t N, F &&f) {
     using std::bool_constant;
     using std::integral_constant;
-    const auto with = [&](auto ns, auto c) { return N == 4 * ns() ? f(ns, c, bool_constant<false>{}) : f(ns, c, bool_constant<true>{}); };
+    const auto with = [&](auto ns, auto c) { return N == 4 * ns() && K % (16 * c()) == 0 ? f(ns, c, bool_constant<false>{}) : f(ns, c, bool_constant<true>{}); };
     if (p.states == 16) return with(integral_constant<int, 16>{}, integral_constant<int, 1>{});
     if (p.channels == 2) return p.states == 4 ? with(integral_constant<int, 4>{}, integral_constant<int, 2>{}) : with(integral_constant<int, 1>{}, integral_constant<int, 2>{});
     return p.states == 4 ? with(integral_constant<int, 4>{}, integral_constant<int, 1>{}) : with(integral_constant<int, 1>{}, integral_constant<int, 1>{});
@@ -81,33 +81,62 @@ inline bool scan_sizes(int64_t B, int64_t L, int64_t K, int64_t N) {
            B * ceil_div(K, 16) <= kMaxTokenRows / 64;
 }
 
-// b or c of one tile, as the lanes of a wavefront load it and keep it in LDS: [kTile][kStates] floats, zero behind N and
-// behind the last token
-template <int NS, typename T>
-__device__ __forceinline__ void load_states(const Tokens<T> &v, int b, int64_t t0, int64_t t1, int N, T (&raw)[NS]) {
+// Addresses of a tile are its first token's, the same for all lanes, and a lane's own 32-bit offset from there: 64-bit ones for
+// every lane and matrix would be kept in registers.  (Pitches are below kMaxPitch for it.)
+constexpr int64_t kMaxPitch = (int64_t)1 << 26;
+template <typename T>
+__device__ __forceinline__ T *in_tile(const Tokens<T> &v, int b, int64_t t0, int token, int column) {
+    return v.at(b, t0) + (token * (int)v.token + column);
+}
+// b or c of one tile: a lane loads NS states of one token, and keeps them in LDS ([kTile][kStates] floats), zero behind N and
+// behind the last token.
+template <int NS, bool RAGGED, typename T>
+__device__ __forceinline__ void load_states(const Tokens<T> &v, int b, int64_t t0, int last, int N, T (&raw)[NS]) {
+    const int lane = threadIdx.x & 63, n0 = (lane & 3) * NS;
+    const T *const from = in_tile(v, b, t0, min(lane >> 2, last), n0);
+    if constexpr (RAGGED)
+        load_first<NS>(from, max(0, min(NS, N - n0)), raw);
+    else
+        load_whole<NS>(from, raw);
+    if (lane >> 2 > last)
 #pragma unroll
-    for (int i = 0; i < NS; i++) {
-        const int at = i * 64 + (threadIdx.x & 63), t = at / (4 * NS), n = at % (4 * NS);
-        raw[i] = t0 + t < t1 && n < N ? v.at(b, t0 + t)[n] : (T)0.0f;
-    }
+        for (int i = 0; i < NS; i++) raw[i] = (T)0.0f;
 }
 template <int NS, typename T>
 __device__ __forceinline__ void keep_states(const T (&raw)[NS], float (*to)[4 * NS]) {
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < NS; i++) {
-        const int at = i * 64 + (threadIdx.x & 63);
-        to[at / (4 * NS)][at % (4 * NS)] = (float)raw[i];
-    }
+    for (int i = 0; i < NS; i++) to[lane >> 2][(lane & 3) * NS + i] = (float)raw[i];
+}
+// V channels from column k on, n of them inside K, of a tile's token; behind the tile's last token the last one's
+template <int V, bool RAGGED, typename T>
+__device__ __forceinline__ void load_token(const Tokens<T> &v, int b, int64_t t0, int token, int last, int k, int n, T (&raw)[V]) {
+    const T *const from = in_tile(v, b, t0, min(token, last), k);
+    if constexpr (RAGGED)
+        load_first<V>(from, n, raw);
+    else
+        load_whole<V>(from, raw);
+}
+template <int V, bool RAGGED, typename T>
+__device__ __forceinline__ void store_token(const Tokens<T> &v, int b, int64_t t0, int token, int k, int n, const float (&out)[V]) {
+    store_first<V>(in_tile(v, b, t0, token, k), RAGGED ? n : V, out);
 }
 
-// NS states of one channel in a [.., K, N] array
-template <int NS>
-__device__ __forceinline__ void load_channel(const float *p, int n0, int N, float (&v)[NS]) {
-    load_first<NS>(p + n0, max(0, min(NS, N - n0)), v);
+// NS states of one channel in a [.., K, N] array; `there`: the channel is one of K
+template <int NS, bool RAGGED>
+__device__ __forceinline__ void load_channel(const float *p, int64_t channel, int n0, int N, bool there, float (&v)[NS]) {
+    if constexpr (RAGGED)
+        load_first<NS>(p + (there ? channel : 0) * N + n0, there ? max(0, min(NS, N - n0)) : 0, v);
+    else
+        load_whole<NS>(p + channel * (4 * NS) + n0, v);
 }
-template <int NS>
-__device__ __forceinline__ void store_channel(float *p, int n0, int N, const float (&v)[NS]) {
-    store_first<NS>(p + n0, max(0, min(NS, N - n0)), v);
+template <int NS, bool RAGGED>
+__device__ __forceinline__ void store_channel(float *p, int64_t channel, int n0, int N, bool there, const float (&v)[NS]) {
+    if constexpr (RAGGED) {
+        if (there) store_first<NS>(p + channel * N + n0, max(0, min(NS, N - n0)), v);
+    } else {
+        store_first<NS>(p + channel * (4 * NS) + n0, NS, v);
+    }
 }
 
 }  // namespace ptq4vm

@@ -13,19 +13,19 @@ namespace {
 
 using namespace ptq4vm;
 
+constexpr int kAhead = 8;  // chunks whose carries are loaded together
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // CARRY_ONLY: from a zero gradient behind the chunk, without outputs; leaves e^{D a} g at the chunk's first token and the sum
 // of D, from which the chunks before it know the gradient that comes in.
-template <typename T, int NS, int C, bool PADDED, bool CARRY_ONLY>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void gated_scan_backward_tokens(ScanArgs<T> p) {
+template <typename T, int NS, int C, bool RAGGED, bool CARRY_ONLY>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 1 : CARRY_ONLY ? 4 : 2))) void gated_scan_backward_tokens(ScanArgs<T> p) {
     using S = ScanLane<NS, C>;
-    static_assert(S::kPasses == 1, "a lane loads one token of a tile");
-    constexpr int kSub = NS * C >= 16 ? 8 : 16;  // tokens whose states are in registers: 128 of them
-    __shared__ float2 steps[kTile][S::kChannels];  // D and D u; then sum g b and sum w a log2(e)
-    __shared__ float grad[kTile][S::kChannels];    // G; then s without d u
-    __shared__ float sb[kTile][S::kStates], sc[kTile][S::kStates];
-    __shared__ float bc[CARRY_ONLY ? 1 : kTile][4][2][S::kStates];  // db and dc of each row of 16 lanes
+    constexpr int kSub = NS * C >= 8 ? 8 : 16;  // tokens whose states are in registers
+    alignas(16) __shared__ float2 steps[kTile][S::kChannels];  // D and D u; then sum g b and sum w a log2(e)
+    alignas(16) __shared__ float grad[kTile][S::kChannels];    // G; then s without d u
+    alignas(16) __shared__ float sb[kTile][S::kStates], sc[kTile][S::kStates];
+    alignas(16) __shared__ float bc[CARRY_ONLY ? 1 : kSub][4][2][S::kStates];  // db and dc of each row of 16 lanes
     const uint32_t block = xcd_contiguous(blockIdx.x, p.blocks);
     if (block >= p.blocks) return;
     const int cb = block % p.column_blocks, from = block / p.column_blocks, b = from % p.B;
@@ -34,81 +34,76 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void ga
     const int64_t t_begin = chunk * p.chunk_tokens, t_end = min(p.L, t_begin + p.chunk_tokens);
 
     float a2[C][NS], carry[C][NS], da[C][NS], sum_d[C];
+    const int kc = cb * S::kChannels + cl * C;  // the quad's first channel
 #pragma unroll
     for (int c = 0; c < C; c++) {
-        const int k = cb * S::kChannels + cl * C + c, n = k < p.K ? p.N : 0;
-        load_channel<NS>(p.a + (int64_t)(n ? k : 0) * p.N, n0, n, a2[c]);
+        const bool mine = !RAGGED || kc + c < p.K;
+        load_channel<NS, RAGGED>(p.a, kc + c, n0, p.N, mine, a2[c]);
         sum_d[c] = 0.0f;
 #pragma unroll
         for (int i = 0; i < NS; i++) a2[c][i] *= kLog2e, carry[c][i] = da[c][i] = 0.0f;
         if constexpr (!CARRY_ONLY)
-            for (uint32_t i = p.chunks - 1; i > chunk; i--) {
-                const int64_t at = n ? ((int64_t)i * p.B + b) * p.K + k : 0;
-                float end[NS];
-                load_channel<NS>(p.chunk_state + at * p.N, n0, n, end);
-                const float D = n ? p.chunk_dt[at] : 0.0f;
+            for (uint32_t i = p.chunks - 1; i > chunk; i -= min(i, (uint32_t)kAhead)) {
+                float end[kAhead][NS], D[kAhead];
 #pragma unroll
-                for (int j = 0; j < NS; j++) carry[c][j] = fmaf(__builtin_amdgcn_exp2f(a2[c][j] * D), carry[c][j], end[j]);
+                for (int s = 0; s < kAhead; s++) {
+                    const uint32_t from = i > chunk + s ? i - s : chunk + 1;
+                    const int64_t channel = ((int64_t)from * p.B + b) * p.K + (mine ? kc + c : 0);
+                    load_channel<NS, RAGGED>(p.chunk_state, channel, n0, p.N, mine, end[s]);
+                    D[s] = p.chunk_dt[channel];
+                }
+#pragma unroll
+                for (int s = 0; s < kAhead; s++)
+                    if (i > chunk + s)
+#pragma unroll
+                        for (int j = 0; j < NS; j++) carry[c][j] = fmaf(__builtin_amdgcn_exp2f(a2[c][j] * D[s]), carry[c][j], end[s][j]);
             }
     }
 
     const int vt = lane / S::kAcross, vk = (lane % S::kAcross) * S::kVec, k = cb * S::kChannels + vk, nk = max(0, min(S::kVec, p.K - k));
-    float bias[S::kVec], skip[S::kVec], dd[S::kVec], dbias[S::kVec];
-#pragma unroll
-    for (int i = 0; i < S::kVec; i++) {
-        bias[i] = p.dt_bias && i < nk ? p.dt_bias[k + i] : 0.0f;
-        skip[i] = p.d && i < nk ? p.d[k + i] : 0.0f;
-        dd[i] = dbias[i] = 0.0f;
+    alignas(16) __shared__ float bias[S::kChannels], skip[S::kChannels];
+    if (lane < S::kChannels) {
+        const int at = cb * S::kChannels + lane;
+        bias[lane] = p.dt_bias && at < p.K ? p.dt_bias[at] : 0.0f;
+        skip[lane] = p.d && at < p.K ? p.d[at] : 0.0f;
     }
-    T ru[S::kVec], rdt[S::kVec], rz[S::kVec], rdy[S::kVec], rb[NS], rc[NS];
-    float h0[C][NS];
-    const auto fetch = [&](int64_t t0) {
-        const int n = t0 + vt < t_end ? nk : 0;
-        const int64_t t = n ? t0 + vt : 0;
-        load_first<S::kVec>(p.dt.at(b, t) + k, n, rdt);
-        load_first<S::kVec>(p.dy.at(b, t) + k, n, rdy);
-        if (p.z.data) load_first<S::kVec>(p.z.at(b, t) + k, n, rz);
-        load_states<NS>(p.c, b, t0, t_end, p.N, rc);
-        if constexpr (!CARRY_ONLY) {
-            load_first<S::kVec>(p.u.at(b, t) + k, n, ru);
-            load_states<NS>(p.b, b, t0, t_end, p.N, rb);
+    __syncthreads();
+    // a lane's sums of dd and ddt_bias (in LDS: read and written once a tile, they would take 16 registers)
+    alignas(16) __shared__ float over_tokens[2][S::kVec / 4][CARRY_ONLY ? 1 : 64][4];
+    if constexpr (!CARRY_ONLY)
 #pragma unroll
-            for (int c = 0; c < C; c++) {
-                const int kc = cb * S::kChannels + cl * C + c;
-                load_channel<NS>(p.marks + (((t0 / kTile) * p.B + b) * p.K + (kc < p.K ? kc : 0)) * p.N, n0, kc < p.K ? p.N : 0, h0[c]);
-            }
-        }
-    };
-    int64_t t0 = t_begin + (t_end - t_begin - 1) / kTile * kTile;
-    fetch(t0);
-    for (; t0 >= t_begin; t0 -= kTile) {
+        for (int i = 0; i < S::kVec; i++) over_tokens[0][i / 4][lane][i % 4] = over_tokens[1][i / 4][lane][i % 4] = 0.0f;
+    for (int64_t t0 = t_begin + (t_end - t_begin - 1) / kTile * kTile; t0 >= t_begin; t0 -= kTile) {
         const bool there = t0 + vt < t_end;  // tokens behind the last change nothing: D, D u, G, b and c are 0
-        float u[S::kVec], D[S::kVec], G[S::kVec], z[S::kVec], dy[S::kVec], slope[S::kVec];
+        T u[S::kVec], dt[S::kVec], z[S::kVec], dy[S::kVec], rb[NS], rc[NS];
+        float start[C][NS], D[S::kVec];
+        const int last = (int)min((int64_t)kTile, t_end - t0) - 1;
+        load_token<S::kVec, RAGGED>(p.dt, b, t0, vt, last, k, nk, dt);
+        load_token<S::kVec, RAGGED>(p.dy, b, t0, vt, last, k, nk, dy);
+        if (p.z.data) load_token<S::kVec, RAGGED>(p.z, b, t0, vt, last, k, nk, z);
+        load_states<NS, RAGGED>(p.c, b, t0, last, p.N, rc);
+        if constexpr (!CARRY_ONLY) {
+            load_token<S::kVec, RAGGED>(p.u, b, t0, vt, last, k, nk, u);
+            load_states<NS, RAGGED>(p.b, b, t0, last, p.N, rb);
+#pragma unroll
+            for (int c = 0; c < C; c++)
+                load_channel<NS, RAGGED>(p.marks, ((t0 / kTile) * p.B + b) * p.K + kc + c, n0, p.N, kc + c < p.K, start[c]);
+        }
 #pragma unroll
         for (int i = 0; i < S::kVec; i++) {
-            const float x = (float)rdt[i] + bias[i];
-            D[i] = there ? softplus_of(x) : 0.0f;
-            slope[i] = sigmoid_of(x);
-            dy[i] = (float)rdy[i];
-            G[i] = dy[i];
-            if (p.z.data) {
-                z[i] = (float)rz[i];
-                G[i] *= z[i] * sigmoid_of(z[i]);
-            }
-            G[i] = there ? G[i] : 0.0f;
-            u[i] = CARRY_ONLY ? 0.0f : (float)ru[i];
-            steps[vt][vk + i] = {D[i], there ? D[i] * u[i] : 0.0f};
-            grad[vt][vk + i] = G[i];
+            D[i] = softplus_of((float)dt[i] + bias[vk + i]);
+            steps[vt][vk + i] = {D[i], CARRY_ONLY ? 0.0f : D[i] * (float)u[i]};
+            grad[vt][vk + i] = (float)dy[i];
         }
+        if (p.z.data)
+#pragma unroll
+            for (int i = 0; i < S::kVec; i++) grad[vt][vk + i] = (float)dy[i] * ((float)z[i] * sigmoid_of((float)z[i]));
+        if (!there)
+#pragma unroll
+            for (int i = 0; i < S::kVec; i++) steps[vt][vk + i] = {0.0f, 0.0f}, grad[vt][vk + i] = 0.0f;
         keep_states<NS>(rc, sc);
         if constexpr (!CARRY_ONLY) keep_states<NS>(rb, sb);
         __syncthreads();
-        float start[C][NS];
-#pragma unroll
-        for (int c = 0; c < C; c++)
-#pragma unroll
-            for (int i = 0; i < NS; i++) start[c][i] = CARRY_ONLY ? 0.0f : h0[c][i];
-        if (t0 > t_begin) fetch(t0 - kTile);
         if constexpr (CARRY_ONLY) {
             for (int t = kTile - 1; t >= 0; t--)
 #pragma unroll
@@ -118,97 +113,131 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void ga
 #pragma unroll
                     for (int i = 0; i < NS; i++) {
                         carry[c][i] = __builtin_amdgcn_exp2f(a2[c][i] * D_t) * fmaf(sc[t][n0 + i], G_t, carry[c][i]);
-                        if (PADDED) carry[c][i] = n0 + i < p.N ? carry[c][i] : 0.0f;
+                        if (RAGGED) carry[c][i] = n0 + i < p.N ? carry[c][i] : 0.0f;
                     }
                 }
             __syncthreads();
             continue;
         }
+        struct Token {
+            float b[NS], c[NS], G[C];
+            float2 D[C];
+        };
+        const auto token_at = [&](int t, int n0, int ch) {
+            Token v;
+#pragma unroll
+            for (int i = 0; i < NS; i++) v.b[i] = sb[t][n0 + i], v.c[i] = sc[t][n0 + i];
+#pragma unroll
+            for (int c = 0; c < C; c++) v.D[c] = steps[t][ch + c], v.G[c] = grad[t][ch + c];
+            return v;
+        };
+        // The same places behind the compiler's back: values and exponentials that it knew from the pass forwards it would keep
+        // through the pass backwards, and they do not fit the registers
+        int n0_again = n0, ch_again = cl * C;
+        asm("" : "+v"(n0_again), "+v"(ch_again));
+        const auto token = [&](int t) { return token_at(t, n0, cl * C); };
+        const auto token_again = [&](int t) { return token_at(t, n0_again, ch_again); };
         for (int sub = kTile - kSub; sub >= 0; sub -= kSub) {
             float h[kSub + 1][C][NS];
-            const auto advance = [&](int t, const float (&before)[C][NS], float (&after)[C][NS]) {
+            const auto advance = [&](const Token &v, const float (&before)[C][NS], float (&after)[C][NS]) {
 #pragma unroll
-                for (int c = 0; c < C; c++) {
-                    const float2 D_t = steps[t][cl * C + c];
+                for (int c = 0; c < C; c++)
 #pragma unroll
                     for (int i = 0; i < NS; i++) {
-                        after[c][i] = fmaf(__builtin_amdgcn_exp2f(a2[c][i] * D_t.x), before[c][i], D_t.y * sb[t][n0 + i]);
-                        if (PADDED) after[c][i] = n0 + i < p.N ? after[c][i] : 0.0f;
+                        after[c][i] = fmaf(__builtin_amdgcn_exp2f(a2[c][i] * v.D[c].x), before[c][i], v.D[c].y * v.b[i]);
+                        if (RAGGED) after[c][i] = n0 + i < p.N ? after[c][i] : 0.0f;
                     }
-                }
             };
 #pragma unroll
             for (int c = 0; c < C; c++)
 #pragma unroll
                 for (int i = 0; i < NS; i++) h[0][c][i] = start[c][i];
-            for (int t = 0; t < sub; t++) advance(t, h[0], h[0]);
+            // the next token's values are read under this one's arithmetic, and no earlier: more would not fit the registers
+            Token next = token(0);
+            for (int t = 0; t < sub; t++) {
+                const Token v = next;
+                next = token(t + 1);
+                advance(v, h[0], h[0]);
+            }
 #pragma unroll
-            for (int s = 0; s < kSub; s++) advance(sub + s, h[s], h[s + 1]);
+            for (int s = 0; s < kSub; s++) {
+                const Token v = next;
+                if (s + 1 < kSub) next = token(sub + s + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                advance(v, h[s], h[s + 1]);
+            }
+            next = token_again(sub + kSub - 1);
 #pragma unroll
             for (int s = kSub - 1; s >= 0; s--) {
                 const int t = sub + s;
-                float gb[C], wa[C], v[C], db[NS], dc[NS];
+                const Token v = next;
+                if (s > 0) next = token_again(t - 1);
+                __builtin_amdgcn_sched_barrier(0);
+                float gb[C], wa[C], out[C], db[NS], dc[NS];
 #pragma unroll
                 for (int i = 0; i < NS; i++) db[i] = dc[i] = 0.0f;
 #pragma unroll
                 for (int c = 0; c < C; c++) {
-                    const float2 D_t = steps[t][cl * C + c];
-                    const float G_t = grad[t][cl * C + c];
-                    gb[c] = wa[c] = v[c] = 0.0f;
+                    gb[c] = wa[c] = out[c] = 0.0f;
 #pragma unroll
                     for (int i = 0; i < NS; i++) {
-                        const float g = fmaf(sc[t][n0 + i], G_t, carry[c][i]);
-                        v[c] = fmaf(sc[t][n0 + i], h[s + 1][c][i], v[c]);
-                        dc[i] = fmaf(h[s + 1][c][i], G_t, dc[i]);
-                        db[i] = fmaf(g, D_t.y, db[i]);
-                        gb[c] = fmaf(g, sb[t][n0 + i], gb[c]);
-                        carry[c][i] = g * __builtin_amdgcn_exp2f(a2[c][i] * D_t.x);
-                        if (PADDED) carry[c][i] = n0 + i < p.N ? carry[c][i] : 0.0f;
+                        const float g = fmaf(v.c[i], v.G[c], carry[c][i]);
+                        out[c] = fmaf(v.c[i], h[s + 1][c][i], out[c]);
+                        dc[i] = fmaf(h[s + 1][c][i], v.G[c], dc[i]);
+                        db[i] = fmaf(g, v.D[c].y, db[i]);
+                        gb[c] = fmaf(g, v.b[i], gb[c]);
+                        carry[c][i] = g * __builtin_amdgcn_exp2f(a2[c][i] * v.D[c].x);
+                        if (RAGGED) carry[c][i] = n0 + i < p.N ? carry[c][i] : 0.0f;
                         const float w = carry[c][i] * h[s][c][i];
                         wa[c] = fmaf(w, a2[c][i], wa[c]);
-                        da[c][i] = fmaf(w, D_t.x, da[c][i]);
+                        da[c][i] = fmaf(w, v.D[c].x, da[c][i]);
                     }
-                    gb[c] = quad_sum(gb[c]);
-                    wa[c] = quad_sum(wa[c]);
-                    v[c] = quad_sum(v[c]);
                 }
-                // (a lane's own reads of this token are done, and so are its quad's: one wavefront, LDS in order)
-                if (q < C) {
-                    const bool second = C == 2 && q == 1;
-                    steps[t][cl * C + q] = {second ? gb[C - 1] : gb[0], second ? wa[C - 1] : wa[0]};
-                    grad[t][cl * C + q] = second ? v[C - 1] : v[0];
-                }
+                // a lane's own reads of this token are done, and so are its quad's: one wavefront, LDS in order (and lanes of the same
+                // place write the same values)
+                steps[t][cl * C + q % C] = {quad_sums<C>(gb, q), quad_sums<C>(wa, q)};
+                grad[t][cl * C + q % C] = quad_sums<C>(out, q);
 #pragma unroll
                 for (int i = 0; i < NS; i++) {  // over the four quads of a row of 16 lanes
                     db[i] = add_dpp<0x128>(add_dpp<0x124>(db[i]));
                     dc[i] = add_dpp<0x128>(add_dpp<0x124>(dc[i]));
-                    if ((lane & 12) == 0) bc[t][lane >> 4][0][n0 + i] = db[i], bc[t][lane >> 4][1][n0 + i] = dc[i];
                 }
+                __builtin_memcpy(&bc[s][lane >> 4][0][n0], db, sizeof(db));
+                __builtin_memcpy(&bc[s][lane >> 4][1][n0], dc, sizeof(dc));
             }
-        }
-        __syncthreads();
+            __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kTile * 2 * S::kStates / 64; j++) {
-            const int at = j * 64 + lane, t = at / (2 * S::kStates), which = at / S::kStates % 2, n = at % S::kStates;
-            const float v = (bc[t][0][which][n] + bc[t][1][which][n]) + (bc[t][2][which][n] + bc[t][3][which][n]);
-            if (t0 + t < t_end && n < p.N) p.partial_bc[((((int64_t)cb * p.B + b) * p.L + t0 + t) * 2 + which) * p.N + n] = v;
-        }
-        float du[S::kVec], ddt[S::kVec], dz[S::kVec];
-#pragma unroll
-        for (int i = 0; i < S::kVec; i++) {
-            const float2 sums = steps[vt][vk + i];
-            du[i] = fmaf(skip[i], G[i], D[i] * sums.x);
-            ddt[i] = fmaf(u[i], sums.x, sums.y * kLn2) * slope[i];
-            if (p.z.data) {
-                const float g = sigmoid_of(z[i]);
-                dz[i] = dy[i] * fmaf(skip[i], u[i], grad[vt][vk + i]) * (g * fmaf(z[i], 1.0f - g, 1.0f));
+            for (int j = 0; j < kSub * 2 * S::kStates / 64; j++) {
+                const int at = j * 64 + lane, s = at / (2 * S::kStates), which = at / S::kStates % 2, n = at % S::kStates;
+                const float v = (bc[s][0][which][n] + bc[s][1][which][n]) + (bc[s][2][which][n] + bc[s][3][which][n]);
+                if (t0 + sub + s < t_end && (!RAGGED || n < p.N)) p.partial_bc[((((int64_t)cb * p.B + b) * p.L + t0 + sub + s) * 2 + which) * (RAGGED ? p.N : S::kStates) + n] = v;
             }
-            if (there && i < nk) dd[i] = fmaf(G[i], u[i], dd[i]), dbias[i] += ddt[i];
+            __syncthreads();
         }
-        if (there && nk) {
-            store_first<S::kVec>(p.du.at(b, t0 + vt) + k, nk, du);
-            store_first<S::kVec>(p.ddt.at(b, t0 + vt) + k, nk, ddt);
-            if (p.z.data) store_first<S::kVec>(p.dz.at(b, t0 + vt) + k, nk, dz);
+        float G[S::kVec], out[S::kVec];
+#pragma unroll
+        for (int i = 0; i < S::kVec; i++) G[i] = (float)dy[i];
+        if (p.z.data) {
+#pragma unroll
+            for (int i = 0; i < S::kVec; i++) {
+                const float g = sigmoid_of((float)z[i]), zg = (float)z[i] * g;
+                out[i] = G[i] * fmaf(skip[vk + i], (float)u[i], grad[vt][vk + i]) * fmaf(zg, 1.0f - g, g);
+                G[i] *= zg;
+            }
+            if (there) store_token<S::kVec, RAGGED>(p.dz, b, t0, vt, k, nk, out);
+        }
+        if (there) {
+#pragma unroll
+            for (int i = 0; i < S::kVec; i++) out[i] = fmaf(skip[vk + i], G[i], D[i] * steps[vt][vk + i].x);
+            store_token<S::kVec, RAGGED>(p.du, b, t0, vt, k, nk, out);
+#pragma unroll
+            for (int i = 0; i < S::kVec; i++) {
+                const float2 sums = steps[vt][vk + i];
+                out[i] = fmaf((float)u[i], sums.x, sums.y * kLn2) * sigmoid_of((float)dt[i] + bias[vk + i]);
+                over_tokens[0][i / 4][lane][i % 4] += G[i] * (float)u[i];
+                over_tokens[1][i / 4][lane][i % 4] += out[i];
+            }
+            store_token<S::kVec, RAGGED>(p.ddt, b, t0, vt, k, nk, out);
         }
         __syncthreads();
     }
@@ -216,23 +245,22 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(2))) void ga
     float *const sums = CARRY_ONLY ? nullptr : p.partial_a + rows * p.K * (p.N + 2);
 #pragma unroll
     for (int c = 0; c < C; c++) {
-        const int kc = cb * S::kChannels + cl * C + c;
-        if (kc >= p.K) continue;
         if constexpr (CARRY_ONLY) {
-            store_channel<NS>(p.chunk_state + (rows * p.K + kc) * p.N, n0, p.N, carry[c]);
-            if (q == 0) p.chunk_dt[rows * p.K + kc] = sum_d[c];
+            store_channel<NS, RAGGED>(p.chunk_state, rows * p.K + kc + c, n0, p.N, kc + c < p.K, carry[c]);
+            if (q == 0 && kc + c < p.K) p.chunk_dt[rows * p.K + kc + c] = sum_d[c];
         } else {
-            store_channel<NS>(sums + (int64_t)kc * p.N, n0, p.N, da[c]);
+            store_channel<NS, RAGGED>(sums, kc + c, n0, p.N, kc + c < p.K, da[c]);
         }
     }
     if constexpr (!CARRY_ONLY) {
         static_assert(S::kAcross == 4, "lanes of the same remainder by 4 hold the same channels");
+        float dd[S::kVec], dbias[S::kVec];
 #pragma unroll
         for (int i = 0; i < S::kVec; i++) {
-            dd[i] = add_dpp<0x128>(add_dpp<0x124>(dd[i]));
+            dd[i] = add_dpp<0x128>(add_dpp<0x124>(over_tokens[0][i / 4][lane][i % 4]));
             dd[i] += __shfl_xor(dd[i], 16, 64);
             dd[i] += __shfl_xor(dd[i], 32, 64);
-            dbias[i] = add_dpp<0x128>(add_dpp<0x124>(dbias[i]));
+            dbias[i] = add_dpp<0x128>(add_dpp<0x124>(over_tokens[1][i / 4][lane][i % 4]));
             dbias[i] += __shfl_xor(dbias[i], 16, 64);
             dbias[i] += __shfl_xor(dbias[i], 32, 64);
         }
@@ -294,6 +322,8 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
     if (!scan_sizes(B, L, K, N)) return PTQ4VM_ERR_SHAPE;
     if (lddy < K || ldu < K || lddt < K || ldb < N || ldc < N || (z && (ldz < K || lddz < K)) || lddu < K || ldddt < K || lddb < N || lddc < N)
         return PTQ4VM_ERR_STRIDE;
+    for (const int64_t ld : {lddy, ldu, lddt, ldb, ldc, z ? ldz : 0, lddu, ldddt, lddb, lddc, z ? lddz : 0})
+        if (ld >= kMaxPitch) return PTQ4VM_ERR_STRIDE;
     const int64_t need = ptq4vm_gated_scan_backward_workspace(B, L, K, N);
     if (need > 0 && !workspace) return PTQ4VM_ERR_NULL;
     if (workspace_bytes < need) return PTQ4VM_ERR_SHAPE;
@@ -321,10 +351,10 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
         s.partial_bc = ws, s.partial_a = ws + sizes.bc, s.chunk_state = s.partial_a + sizes.a, s.chunk_dt = s.chunk_state + (sizes.chunk ? plan.chunks * B * K * N : 0);
         s.B = (int)B, s.K = (int)K, s.N = (int)N, s.column_blocks = (int)plan.column_blocks, s.L = L, s.chunk_tokens = plan.chunk_tokens;
         s.chunks = (uint32_t)plan.chunks;
-        const int e2 = for_layout(plan, N, [&](auto ns, auto ch, auto padded) {
+        const int e2 = for_layout(plan, K, N, [&](auto ns, auto ch, auto ragged) {
             const auto go = [&](auto carry_only, int64_t chunks) {
                 s.blocks = (uint32_t)(chunks * B * plan.column_blocks);
-                gated_scan_backward_tokens<T, ns(), ch(), padded(), carry_only()><<<dim3(xcd_grid(s.blocks)), dim3(64), 0, stream>>>(s);
+                gated_scan_backward_tokens<T, ns(), ch(), ragged(), carry_only()><<<dim3(xcd_grid(s.blocks)), dim3(64), 0, stream>>>(s);
                 return check_launch("gated_scan_backward_tokens");
             };
             if (plan.chunks > 1)

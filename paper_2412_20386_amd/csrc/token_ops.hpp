@@ -74,30 +74,29 @@ __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f
 // 1 / (1 + e^-v): 0 and 1 at the infinities, NaN for a NaN
 __device__ __forceinline__ float sigmoid_of(float v) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-v)); }
 
-// ln(1 + e^v) = max(v, 0) + ln(1 + e), e = e^-|v| in [0, 1], and ln(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3: a series in
-// s^2 <= 1/9 whose first left-out term is 9^-8 / 17 = 1.4e-9 of the result.  No step cancels, so small results (a step size of
-// 0.001 is an input of -7) keep all their digits; ln(1 + e) itself would keep 14 bits of them.
+// ln(1 + e^v) = max(v, 0) + ln(1 + e), e = e^-|v| in [0, 1].  The sum w = 1 + e loses up to 2^-24 of e; what it lost, e - (w - 1),
+// is exact, and added to ln w to first order (its factor 1 / w matters only where ln w is large): small results (a step size
+// of 0.001 is an input of -7) keep all their digits, where ln w alone would keep 14 bits.
 __device__ __forceinline__ float softplus_of(float v) {
-    const float e = exp_of(-fabsf(v));
-    const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
-    float p = 1.0f / 15;
-    p = fmaf(p, q, 1.0f / 13);
-    p = fmaf(p, q, 1.0f / 11);
-    p = fmaf(p, q, 1.0f / 9);
-    p = fmaf(p, q, 1.0f / 7);
-    p = fmaf(p, q, 1.0f / 5);
-    p = fmaf(p, q, 1.0f / 3);
-    p = fmaf(p, q, 1.0f);
-    return fmaf(s + s, p, fmaxf(v, 0.0f));
+    const float e = exp_of(-fabsf(v)), w = 1.0f + e;
+    return fmaxf(v, 0.0f) + fmaf(__builtin_amdgcn_logf(w), 0.69314718055994530942f, e - (w - 1.0f));
 }
 
 // v + v of another lane of the row of 16, a VALU instruction
 template <int CTRL>
 __device__ __forceinline__ float add_dpp(float v) {
-    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
 // Sum over the 4 lanes of a quad, in every lane of it
 __device__ __forceinline__ float quad_sum(float v) { return add_dpp<0x4E>(add_dpp<0xB1>(v)); }
+// Sums over the lanes of a quad of C values each: in lane q that of value q modulo C
+template <int C>
+__device__ __forceinline__ float quad_sums(const float (&v)[C], int q) {
+    static_assert(C == 1 || C == 2, "one value or two");
+    if constexpr (C == 1) return quad_sum(v[0]);
+    const float mine = q & 1 ? v[C - 1] : v[0], other = q & 1 ? v[0] : v[C - 1];
+    return add_dpp<0x4E>(mine + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, other), 0xB1, 0xf, 0xf, true)));
+}
 // Sum over an aligned group of `lanes` = 2^n lanes, in every lane of it
 __device__ __forceinline__ float group_sum(float v, int lanes) {
     if (lanes >= 2) v = add_dpp<0xB1>(v);    // quad_perm 1,0,3,2
