@@ -347,7 +347,7 @@ typedef enum { PTQ4VM_F16 = 0, PTQ4VM_BF16 = 1, PTQ4VM_F32 = 2 } ptq4vm_dtype;
  * Few long sequences are cut into chunks that run side by side (two launches).  Errors: NULL u / dt / a / b / c / y, sizes out of
  * range (N up to PTQ4VM_MAX_SCAN_N), ld* below a row's width, misalignment, workspace too small (PTQ4VM_ERR_SHAPE) or missing.
  */
-#define PTQ4VM_SCAN_TILE 16
+#define PTQ4VM_SCAN_TILE 8
 #define PTQ4VM_SCAN_MARKS(L) ((((int64_t)(L)) + PTQ4VM_SCAN_TILE - 1) / PTQ4VM_SCAN_TILE)
 #define PTQ4VM_MAX_SCAN_N 64
 int64_t ptq4vm_gated_scan_workspace(int64_t B, int64_t L, int64_t K, int64_t N);

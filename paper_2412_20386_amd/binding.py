@@ -280,7 +280,7 @@ def e2m3_blocks(K: int) -> int:
     return (K + 127) // 128
 
 
-SCAN_TILE = 16  # PTQ4VM_SCAN_TILE
+SCAN_TILE = 8  # PTQ4VM_SCAN_TILE
 
 
 def scan_marks(L: int) -> int:

@@ -5,6 +5,7 @@ namespace {
 
 using namespace ptq4vm;
 
+constexpr int kTile = 16;  // tokens that are staged together
 constexpr int kAhead = 8;  // chunks whose states are loaded together
 
 // One wavefront: 16 C channels of one sequence through the tokens of one chunk.
@@ -13,7 +14,7 @@ constexpr int kAhead = 8;  // chunks whose states are loaded together
 // RAGGED: K or N leave lanes without a channel or a state; the states behind N are kept at zero.
 template <typename T, int NS, int C, bool RAGGED, bool STATES_ONLY>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 2 : 4))) void gated_scan_tokens(ScanArgs<T> p) {
-    using S = ScanLane<NS, C>;
+    using S = ScanLane<NS, C, kTile>;
     alignas(16) __shared__ float2 steps[kTile][S::kChannels];  // D and D u
     alignas(16) __shared__ float sums[kTile][S::kChannels];    // s without its d u
     alignas(16) __shared__ float sb[kTile][S::kStates], sc[kTile][S::kStates];
@@ -61,14 +62,14 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
         skip[lane] = p.d && at < p.K ? p.d[at] : 0.0f;
     }
     __syncthreads();
-    T ru[S::kVec], rdt[S::kVec], rz[S::kVec], rb[NS], rc[NS];
+    T ru[S::kVec], rdt[S::kVec], rz[S::kVec], rb[S::kStateVec], rc[S::kStateVec];
     const auto fetch = [&](int64_t t0) {
         const int last = (int)min((int64_t)kTile, t_end - t0) - 1;
         load_token<S::kVec, RAGGED>(p.u, b, t0, vt, last, k, nk, ru);
         load_token<S::kVec, RAGGED>(p.dt, b, t0, vt, last, k, nk, rdt);
         if (!STATES_ONLY && p.z.data) load_token<S::kVec, RAGGED>(p.z, b, t0, vt, last, k, nk, rz);
-        load_states<NS, RAGGED>(p.b, b, t0, last, p.N, rb);
-        if constexpr (!STATES_ONLY) load_states<NS, RAGGED>(p.c, b, t0, last, p.N, rc);
+        load_states<S, RAGGED>(p.b, b, t0, last, p.N, rb);
+        if constexpr (!STATES_ONLY) load_states<S, RAGGED>(p.c, b, t0, last, p.N, rc);
     };
     fetch(t_begin);
     for (int64_t t0 = t_begin; t0 < t_end; t0 += kTile) {
@@ -84,16 +85,17 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
         if (!there)
 #pragma unroll
             for (int i = 0; i < S::kVec; i++) steps[vt][vk + i] = {0.0f, 0.0f};
-        keep_states<NS>(rb, sb);
-        if constexpr (!STATES_ONLY) keep_states<NS>(rc, sc);
+        keep_states<S>(rb, sb);
+        if constexpr (!STATES_ONLY) keep_states<S>(rc, sc);
         __syncthreads();
         if (t0 + kTile < t_end) fetch(t0 + kTile);  // in flight under this tile's steps
-        if (!STATES_ONLY && p.marks)
-#pragma unroll
-            for (int c = 0; c < C; c++)
-                store_channel<NS, RAGGED>(p.marks, ((t0 / kTile) * p.B + b) * p.K + kc + c, n0, p.N, kc + c < p.K, h[c]);
         const int groups = (int)((min((int64_t)kTile, t_end - t0) + 3) / 4);
-        for (int g = 0; g < groups; g++)
+        for (int g = 0; g < groups; g++) {
+            static_assert(kMark == 8 && kTile == 16, "a mark before every other group of four tokens");
+            if (!STATES_ONLY && p.marks && g % 2 == 0)
+#pragma unroll
+                for (int c = 0; c < C; c++)
+                    store_channel<NS, RAGGED>(p.marks, ((t0 / kMark + g / 2) * p.B + b) * p.K + kc + c, n0, p.N, kc + c < p.K, h[c]);
 #pragma unroll
             for (int s = 0; s < 4; s++) {
                 const int t = 4 * g + s;
@@ -117,6 +119,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
                 }
                 if constexpr (!STATES_ONLY) sums[t][cl * C + q % C] = quad_sums<C>(v, q);  // (lanes of the same place write the same value)
             }
+        }
         __syncthreads();
         if constexpr (!STATES_ONLY) {
             float y[S::kVec];

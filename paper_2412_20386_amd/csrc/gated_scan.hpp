@@ -14,7 +14,7 @@
 
 namespace ptq4vm {
 
-constexpr int kTile = PTQ4VM_SCAN_TILE;  // tokens that are staged together; marks are kept for their starts
+constexpr int kMark = PTQ4VM_SCAN_TILE;  // tokens from one mark to the next
 
 template <typename T>
 struct ScanArgs {
@@ -26,18 +26,18 @@ struct ScanArgs {
     Tokens<T> dy, du, ddt, dz;
     float *partial_bc, *partial_a;
     int B, K, N, column_blocks;
-    int64_t L, chunk_tokens;  // (a multiple of kTile)
+    int64_t L, chunk_tokens;  // (a multiple of 16)
     uint32_t chunks, blocks;
 };
 
-// What the layout of a wavefront makes of its lane number
-template <int NS, int C>
+// What the layout of a wavefront makes of its lane number, where TOKENS tokens are staged at once
+template <int NS, int C, int TOKENS>
 struct ScanLane {
-    static constexpr int kChannels = 16 * C;             // of a wavefront
-    static constexpr int kStates = 4 * NS;               // that a quad has room for
-    static constexpr int kVec = C == 1 ? 4 : 8;          // channels that a lane loads of one token
-    static constexpr int kAcross = kChannels / kVec;     // lanes side by side
-    static_assert(64 / kAcross == kTile, "the lanes of a wavefront load a tile at once");
+    static constexpr int kChannels = 16 * C;                // of a wavefront
+    static constexpr int kStates = 4 * NS;                  // that a quad has room for
+    static constexpr int kAcross = 64 / TOKENS;             // lanes side by side that load a token
+    static constexpr int kVec = kChannels / kAcross;        // channels that a lane loads of its token
+    static constexpr int kStateVec = (kStates * TOKENS + 63) / 64;  // states that a lane loads of b and of c
 };
 
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -57,9 +57,9 @@ inline ScanPlan scan_plan(int64_t B, int64_t L, int64_t K, int64_t N) {
     p.column_blocks = ceil_div(K, 16 * p.channels);
     const int64_t waves = B * p.column_blocks;
     int64_t chunks = waves >= 1024 ? 1 : ceil_div(4096, waves > 0 ? waves : 1);
-    if (chunks > ceil_div(L, 2 * kTile)) chunks = ceil_div(L, 2 * kTile);
+    if (chunks > ceil_div(L, 32)) chunks = ceil_div(L, 32);
     if (chunks > 128) chunks = 128;
-    p.chunk_tokens = ceil_div(ceil_div(L, chunks), kTile) * kTile;
+    p.chunk_tokens = ceil_div(ceil_div(L, chunks), 16) * 16;
     p.chunks = ceil_div(L, p.chunk_tokens);
     return p;
 }
@@ -88,25 +88,27 @@ template <typename T>
 __device__ __forceinline__ T *in_tile(const Tokens<T> &v, int b, int64_t t0, int token, int column) {
     return v.at(b, t0) + (token * (int)v.token + column);
 }
-// b or c of one tile: a lane loads NS states of one token, and keeps them in LDS ([kTile][kStates] floats), zero behind N and
-// behind the last token.
-template <int NS, bool RAGGED, typename T>
-__device__ __forceinline__ void load_states(const Tokens<T> &v, int b, int64_t t0, int last, int N, T (&raw)[NS]) {
-    const int lane = threadIdx.x & 63, n0 = (lane & 3) * NS;
-    const T *const from = in_tile(v, b, t0, min(lane >> 2, last), n0);
+// b or c of one tile: a lane loads kStateVec states of one token, and keeps them in LDS ([TOKENS][kStates] floats), zero behind
+// N and behind the last token.  (Where the states are fewer than the lanes, the others repeat them.)
+template <typename S, bool RAGGED, typename T>
+__device__ __forceinline__ void load_states(const Tokens<T> &v, int b, int64_t t0, int last, int N, T (&raw)[S::kStateVec]) {
+    constexpr int V = S::kStateVec, kLanes = S::kStates / V;
+    const int lane = threadIdx.x & 63, token = lane / kLanes % (64 / S::kAcross), n0 = lane % kLanes * V;
+    const T *const from = in_tile(v, b, t0, min(token, last), n0);
     if constexpr (RAGGED)
-        load_first<NS>(from, max(0, min(NS, N - n0)), raw);
+        load_first<V>(from, max(0, min(V, N - n0)), raw);
     else
-        load_whole<NS>(from, raw);
-    if (lane >> 2 > last)
+        load_whole<V>(from, raw);
+    if (token > last)
 #pragma unroll
-        for (int i = 0; i < NS; i++) raw[i] = (T)0.0f;
+        for (int i = 0; i < V; i++) raw[i] = (T)0.0f;
 }
-template <int NS, typename T>
-__device__ __forceinline__ void keep_states(const T (&raw)[NS], float (*to)[4 * NS]) {
+template <typename S, typename T>
+__device__ __forceinline__ void keep_states(const T (&raw)[S::kStateVec], float (*to)[S::kStates]) {
+    constexpr int V = S::kStateVec, kLanes = S::kStates / V;
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < NS; i++) to[lane >> 2][(lane & 3) * NS + i] = (float)raw[i];
+    for (int i = 0; i < V; i++) to[lane / kLanes % (64 / S::kAcross)][lane % kLanes * V + i] = (float)raw[i];
 }
 // V channels from column k on, n of them inside K, of a tile's token; behind the tile's last token the last one's
 template <int V, bool RAGGED, typename T>

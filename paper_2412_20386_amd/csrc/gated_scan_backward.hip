@@ -3,7 +3,7 @@
 //   g_t = c_t G_t + e^{D a} (at t + 1) g_{t+1},  w_t = g_t e^{D a} h_{t-1},
 //   dc_t = sum_k G h_t,  db_t = sum_k g D u,  da = sum_{b,t} w D,  dd = sum G u,  dz = dy s (derivative of the gate),
 //   du = d G + D sum_n g b,  dD = u sum_n g b + sum_n w a,  ddt = dD / (1 + e^-(dt + dt_bias)),  ddt_bias = sum ddt.
-// A wavefront takes its tiles of kTile tokens from the last to the first: the states of a tile are computed again from its
+// A wavefront takes its tiles of kMark tokens from the last to the first: the states of a tile are computed again from its
 // mark into registers, then the tile is run through backwards.  Sums over channels (db, dc) leave a wavefront as one row of
 // 2 N partial sums a token, sums over tokens (da, dd, ddt_bias) as one row for each sequence and chunk; both are summed up
 // in a fixed order by kernels of their own.
@@ -13,6 +13,7 @@ namespace {
 
 using namespace ptq4vm;
 
+constexpr int kTile = kMark;  // tokens that are staged together, and whose states are in registers
 constexpr int kAhead = 8;  // chunks whose carries are loaded together
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -20,12 +21,14 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // of D, from which the chunks before it know the gradient that comes in.
 template <typename T, int NS, int C, bool RAGGED, bool CARRY_ONLY>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 1 : CARRY_ONLY ? 4 : 2))) void gated_scan_backward_tokens(ScanArgs<T> p) {
-    using S = ScanLane<NS, C>;
-    constexpr int kSub = NS * C >= 8 ? 8 : 16;  // tokens whose states are in registers
-    alignas(16) __shared__ float2 steps[kTile][S::kChannels];  // D and D u; then sum g b and sum w a log2(e)
-    alignas(16) __shared__ float grad[kTile][S::kChannels];    // G; then s without d u
+    using S = ScanLane<NS, C, kTile>;
+    constexpr int V = S::kVec;
+    alignas(16) __shared__ float2 steps[kTile][S::kChannels];  // D and D u, then sum g b
+    alignas(16) __shared__ float grad[kTile][S::kChannels];    // G, then sum w a log2(e)
     alignas(16) __shared__ float sb[kTile][S::kStates], sc[kTile][S::kStates];
-    alignas(16) __shared__ float bc[CARRY_ONLY ? 1 : kSub][4][2][S::kStates];  // db and dc of each row of 16 lanes
+    alignas(16) __shared__ float out_sums[CARRY_ONLY ? 1 : kTile][S::kChannels];  // s without d u
+    alignas(16) __shared__ float bc[CARRY_ONLY ? 1 : kTile][2][S::kStates];       // the wavefront's db and dc
+    alignas(16) __shared__ float bias[S::kChannels], skip[S::kChannels];
     const uint32_t block = xcd_contiguous(blockIdx.x, p.blocks);
     if (block >= p.blocks) return;
     const int cb = block % p.column_blocks, from = block / p.column_blocks, b = from % p.B;
@@ -60,50 +63,65 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
             }
     }
 
-    const int vt = lane / S::kAcross, vk = (lane % S::kAcross) * S::kVec, k = cb * S::kChannels + vk, nk = max(0, min(S::kVec, p.K - k));
-    alignas(16) __shared__ float bias[S::kChannels], skip[S::kChannels];
+    // what this lane loads: V channels of a token
+    const int vt = lane / S::kAcross, vk = (lane % S::kAcross) * V, k = cb * S::kChannels + vk, nk = max(0, min(V, p.K - k));
     if (lane < S::kChannels) {
         const int at = cb * S::kChannels + lane;
         bias[lane] = p.dt_bias && at < p.K ? p.dt_bias[at] : 0.0f;
         skip[lane] = p.d && at < p.K ? p.d[at] : 0.0f;
     }
     __syncthreads();
-    // a lane's sums of dd and ddt_bias (in LDS: read and written once a tile, they would take 16 registers)
-    alignas(16) __shared__ float over_tokens[2][S::kVec / 4][CARRY_ONLY ? 1 : 64][4];
-    if constexpr (!CARRY_ONLY)
+    float dd[V], dbias[V];
 #pragma unroll
-        for (int i = 0; i < S::kVec; i++) over_tokens[0][i / 4][lane][i % 4] = over_tokens[1][i / 4][lane][i % 4] = 0.0f;
-    for (int64_t t0 = t_begin + (t_end - t_begin - 1) / kTile * kTile; t0 >= t_begin; t0 -= kTile) {
-        const bool there = t0 + vt < t_end;  // tokens behind the last change nothing: D, D u, G, b and c are 0
-        T u[S::kVec], dt[S::kVec], z[S::kVec], dy[S::kVec], rb[NS], rc[NS];
-        float start[C][NS], D[S::kVec];
+    for (int i = 0; i < V; i++) dd[i] = dbias[i] = 0.0f;
+    T ru[V], rdt[V], rz[V], rdy[V], rb[S::kStateVec], rc[S::kStateVec];
+    float mark[C][NS];
+    const auto fetch = [&](int64_t t0) {
         const int last = (int)min((int64_t)kTile, t_end - t0) - 1;
-        load_token<S::kVec, RAGGED>(p.dt, b, t0, vt, last, k, nk, dt);
-        load_token<S::kVec, RAGGED>(p.dy, b, t0, vt, last, k, nk, dy);
-        if (p.z.data) load_token<S::kVec, RAGGED>(p.z, b, t0, vt, last, k, nk, z);
-        load_states<NS, RAGGED>(p.c, b, t0, last, p.N, rc);
+        load_token<V, RAGGED>(p.dt, b, t0, vt, last, k, nk, rdt);
+        load_token<V, RAGGED>(p.dy, b, t0, vt, last, k, nk, rdy);
+        if (p.z.data) load_token<V, RAGGED>(p.z, b, t0, vt, last, k, nk, rz);
+        load_states<S, RAGGED>(p.c, b, t0, last, p.N, rc);
         if constexpr (!CARRY_ONLY) {
-            load_token<S::kVec, RAGGED>(p.u, b, t0, vt, last, k, nk, u);
-            load_states<NS, RAGGED>(p.b, b, t0, last, p.N, rb);
+            load_token<V, RAGGED>(p.u, b, t0, vt, last, k, nk, ru);
+            load_states<S, RAGGED>(p.b, b, t0, last, p.N, rb);
 #pragma unroll
             for (int c = 0; c < C; c++)
-                load_channel<NS, RAGGED>(p.marks, ((t0 / kTile) * p.B + b) * p.K + kc + c, n0, p.N, kc + c < p.K, start[c]);
+                load_channel<NS, RAGGED>(p.marks, ((t0 / kMark) * p.B + b) * p.K + kc + c, n0, p.N, kc + c < p.K, mark[c]);
         }
+    };
+    int64_t t0 = t_begin + (t_end - t_begin - 1) / kTile * kTile;
+    fetch(t0);
+    for (; t0 >= t_begin; t0 -= kTile) {
+        const bool there = t0 + vt < t_end;  // tokens behind the last change nothing: D, D u, G, b and c are 0
+        T u[V], dt[V], z[V], dy[V];
+        float h[kTile + 1][C][NS];
 #pragma unroll
-        for (int i = 0; i < S::kVec; i++) {
-            D[i] = softplus_of((float)dt[i] + bias[vk + i]);
-            steps[vt][vk + i] = {D[i], CARRY_ONLY ? 0.0f : D[i] * (float)u[i]};
+        for (int i = 0; i < V; i++) {
+            dt[i] = rdt[i], dy[i] = rdy[i], z[i] = rz[i];
+            if constexpr (!CARRY_ONLY) u[i] = ru[i];
+        }
+        if constexpr (!CARRY_ONLY)
+#pragma unroll
+            for (int c = 0; c < C; c++)
+#pragma unroll
+                for (int i = 0; i < NS; i++) h[0][c][i] = mark[c][i];
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const float D = softplus_of((float)dt[i] + bias[vk + i]);
+            steps[vt][vk + i] = {D, CARRY_ONLY ? 0.0f : D * (float)u[i]};
             grad[vt][vk + i] = (float)dy[i];
         }
         if (p.z.data)
 #pragma unroll
-            for (int i = 0; i < S::kVec; i++) grad[vt][vk + i] = (float)dy[i] * ((float)z[i] * sigmoid_of((float)z[i]));
+            for (int i = 0; i < V; i++) grad[vt][vk + i] = (float)dy[i] * ((float)z[i] * sigmoid_of((float)z[i]));
         if (!there)
 #pragma unroll
-            for (int i = 0; i < S::kVec; i++) steps[vt][vk + i] = {0.0f, 0.0f}, grad[vt][vk + i] = 0.0f;
-        keep_states<NS>(rc, sc);
-        if constexpr (!CARRY_ONLY) keep_states<NS>(rb, sb);
+            for (int i = 0; i < V; i++) steps[vt][vk + i] = {0.0f, 0.0f}, grad[vt][vk + i] = 0.0f;
+        keep_states<S>(rc, sc);
+        if constexpr (!CARRY_ONLY) keep_states<S>(rb, sb);
         __syncthreads();
+        if (t0 > t_begin) fetch(t0 - kTile);  // in flight under this tile's steps
         if constexpr (CARRY_ONLY) {
             for (int t = kTile - 1; t >= 0; t--)
 #pragma unroll
@@ -133,111 +151,98 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
         };
         // The same places behind the compiler's back: values and exponentials that it knew from the pass forwards it would keep
         // through the pass backwards, and they do not fit the registers
-        int n0_again = n0, ch_again = cl * C;
-        asm("" : "+v"(n0_again), "+v"(ch_again));
+        int q_again = q, cl_again = cl;
+        asm("" : "+v"(q_again), "+v"(cl_again));
         const auto token = [&](int t) { return token_at(t, n0, cl * C); };
-        const auto token_again = [&](int t) { return token_at(t, n0_again, ch_again); };
-        for (int sub = kTile - kSub; sub >= 0; sub -= kSub) {
-            float h[kSub + 1][C][NS];
-            const auto advance = [&](const Token &v, const float (&before)[C][NS], float (&after)[C][NS]) {
+        const auto token_again = [&](int t) { return token_at(t, q_again * NS, cl_again * C); };
+        // the next token's values are read under this one's arithmetic, and no earlier: more would not fit the registers
+        Token next = token(0);
 #pragma unroll
-                for (int c = 0; c < C; c++)
-#pragma unroll
-                    for (int i = 0; i < NS; i++) {
-                        after[c][i] = fmaf(__builtin_amdgcn_exp2f(a2[c][i] * v.D[c].x), before[c][i], v.D[c].y * v.b[i]);
-                        if (RAGGED) after[c][i] = n0 + i < p.N ? after[c][i] : 0.0f;
-                    }
-            };
+        for (int t = 0; t < kTile; t++) {
+            const Token v = next;
+            next = t + 1 < kTile ? token(t + 1) : token_again(kTile - 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int c = 0; c < C; c++)
 #pragma unroll
-                for (int i = 0; i < NS; i++) h[0][c][i] = start[c][i];
-            // the next token's values are read under this one's arithmetic, and no earlier: more would not fit the registers
-            Token next = token(0);
-            for (int t = 0; t < sub; t++) {
-                const Token v = next;
-                next = token(t + 1);
-                advance(v, h[0], h[0]);
-            }
-#pragma unroll
-            for (int s = 0; s < kSub; s++) {
-                const Token v = next;
-                if (s + 1 < kSub) next = token(sub + s + 1);
-                __builtin_amdgcn_sched_barrier(0);
-                advance(v, h[s], h[s + 1]);
-            }
-            next = token_again(sub + kSub - 1);
-#pragma unroll
-            for (int s = kSub - 1; s >= 0; s--) {
-                const int t = sub + s;
-                const Token v = next;
-                if (s > 0) next = token_again(t - 1);
-                __builtin_amdgcn_sched_barrier(0);
-                float gb[C], wa[C], out[C], db[NS], dc[NS];
-#pragma unroll
-                for (int i = 0; i < NS; i++) db[i] = dc[i] = 0.0f;
-#pragma unroll
-                for (int c = 0; c < C; c++) {
-                    gb[c] = wa[c] = out[c] = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < NS; i++) {
-                        const float g = fmaf(v.c[i], v.G[c], carry[c][i]);
-                        out[c] = fmaf(v.c[i], h[s + 1][c][i], out[c]);
-                        dc[i] = fmaf(h[s + 1][c][i], v.G[c], dc[i]);
-                        db[i] = fmaf(g, v.D[c].y, db[i]);
-                        gb[c] = fmaf(g, v.b[i], gb[c]);
-                        carry[c][i] = g * __builtin_amdgcn_exp2f(a2[c][i] * v.D[c].x);
-                        if (RAGGED) carry[c][i] = n0 + i < p.N ? carry[c][i] : 0.0f;
-                        const float w = carry[c][i] * h[s][c][i];
-                        wa[c] = fmaf(w, a2[c][i], wa[c]);
-                        da[c][i] = fmaf(w, v.D[c].x, da[c][i]);
-                    }
+                for (int i = 0; i < NS; i++) {
+                    h[t + 1][c][i] = fmaf(__builtin_amdgcn_exp2f(a2[c][i] * v.D[c].x), h[t][c][i], v.D[c].y * v.b[i]);
+                    if (RAGGED) h[t + 1][c][i] = n0 + i < p.N ? h[t + 1][c][i] : 0.0f;
                 }
-                // a lane's own reads of this token are done, and so are its quad's: one wavefront, LDS in order (and lanes of the same
-                // place write the same values)
-                steps[t][cl * C + q % C] = {quad_sums<C>(gb, q), quad_sums<C>(wa, q)};
-                grad[t][cl * C + q % C] = quad_sums<C>(out, q);
-#pragma unroll
-                for (int i = 0; i < NS; i++) {  // over the four quads of a row of 16 lanes
-                    db[i] = add_dpp<0x128>(add_dpp<0x124>(db[i]));
-                    dc[i] = add_dpp<0x128>(add_dpp<0x124>(dc[i]));
-                }
-                __builtin_memcpy(&bc[s][lane >> 4][0][n0], db, sizeof(db));
-                __builtin_memcpy(&bc[s][lane >> 4][1][n0], dc, sizeof(dc));
-            }
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < kSub * 2 * S::kStates / 64; j++) {
-                const int at = j * 64 + lane, s = at / (2 * S::kStates), which = at / S::kStates % 2, n = at % S::kStates;
-                const float v = (bc[s][0][which][n] + bc[s][1][which][n]) + (bc[s][2][which][n] + bc[s][3][which][n]);
-                if (t0 + sub + s < t_end && (!RAGGED || n < p.N)) p.partial_bc[((((int64_t)cb * p.B + b) * p.L + t0 + sub + s) * 2 + which) * (RAGGED ? p.N : S::kStates) + n] = v;
-            }
-            __syncthreads();
         }
-        float G[S::kVec], out[S::kVec];
 #pragma unroll
-        for (int i = 0; i < S::kVec; i++) G[i] = (float)dy[i];
-        if (p.z.data) {
+        for (int t = kTile - 1; t >= 0; t--) {
+            const Token v = next;
+            if (t > 0) next = token_again(t - 1);
+            __builtin_amdgcn_sched_barrier(0);
+            float gb[C], wa[C], out[C], db[NS], dc[NS];
 #pragma unroll
-            for (int i = 0; i < S::kVec; i++) {
-                const float g = sigmoid_of((float)z[i]), zg = (float)z[i] * g;
-                out[i] = G[i] * fmaf(skip[vk + i], (float)u[i], grad[vt][vk + i]) * fmaf(zg, 1.0f - g, g);
-                G[i] *= zg;
+            for (int i = 0; i < NS; i++) db[i] = dc[i] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < C; c++) {
+                gb[c] = wa[c] = out[c] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < NS; i++) {
+                    const float g = fmaf(v.c[i], v.G[c], carry[c][i]);
+                    out[c] = fmaf(v.c[i], h[t + 1][c][i], out[c]);
+                    dc[i] = fmaf(h[t + 1][c][i], v.G[c], dc[i]);
+                    db[i] = fmaf(g, v.D[c].y, db[i]);
+                    gb[c] = fmaf(g, v.b[i], gb[c]);
+                    carry[c][i] = g * __builtin_amdgcn_exp2f(a2[c][i] * v.D[c].x);
+                    if (RAGGED) carry[c][i] = n0 + i < p.N ? carry[c][i] : 0.0f;
+                    const float w = carry[c][i] * h[t][c][i];
+                    wa[c] = fmaf(w, a2[c][i], wa[c]);
+                    da[c][i] = fmaf(w, v.D[c].x, da[c][i]);
+                }
             }
-            if (there) store_token<S::kVec, RAGGED>(p.dz, b, t0, vt, k, nk, out);
+            // a lane's own reads of this token are done, and so are its quad's: one wavefront, LDS in order (and lanes of the same
+            // place write the same values)
+            steps[t][cl * C + q % C].y = quad_sums<C>(gb, q);
+            grad[t][cl * C + q % C] = quad_sums<C>(wa, q);
+            out_sums[t][cl * C + q % C] = quad_sums<C>(out, q);
+            // db and dc over the wavefront's channels: halves, rows, then the quads of a row
+            float half[NS];
+#pragma unroll
+            for (int i = 0; i < NS; i++) half[i] = sum_halves(db[i], dc[i]);
+            if constexpr (NS == 1)
+                bc[t][lane >> 5][n0] = sum_quads(sum_rows(half[0], half[0]));
+            else
+#pragma unroll
+                for (int i = 0; i < NS; i += 2) bc[t][lane >> 5][n0 + i + (lane >> 4 & 1)] = sum_quads(sum_rows(half[i], half[i + 1]));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kTile * 2 * S::kStates / 64; j++) {
+            const int at = j * 64 + lane, t = at / (2 * S::kStates), which = at / S::kStates % 2, n = at % S::kStates;
+            if (t0 + t < t_end && (!RAGGED || n < p.N))
+                p.partial_bc[((((int64_t)cb * p.B + b) * p.L + t0 + t) * 2 + which) * (RAGGED ? p.N : S::kStates) + n] = bc[t][which][n];
         }
         if (there) {
+            float G[V], out[V];
 #pragma unroll
-            for (int i = 0; i < S::kVec; i++) out[i] = fmaf(skip[vk + i], G[i], D[i] * steps[vt][vk + i].x);
-            store_token<S::kVec, RAGGED>(p.du, b, t0, vt, k, nk, out);
+            for (int i = 0; i < V; i++) G[i] = (float)dy[i];
+            if (p.z.data) {
 #pragma unroll
-            for (int i = 0; i < S::kVec; i++) {
-                const float2 sums = steps[vt][vk + i];
-                out[i] = fmaf((float)u[i], sums.x, sums.y * kLn2) * sigmoid_of((float)dt[i] + bias[vk + i]);
-                over_tokens[0][i / 4][lane][i % 4] += G[i] * (float)u[i];
-                over_tokens[1][i / 4][lane][i % 4] += out[i];
+                for (int i = 0; i < V; i++) {
+                    const float g = sigmoid_of((float)z[i]), zg = (float)z[i] * g;
+                    out[i] = G[i] * fmaf(skip[vk + i], (float)u[i], out_sums[vt][vk + i]) * fmaf(zg, 1.0f - g, g);
+                    G[i] *= zg;
+                }
+                store_token<V, RAGGED>(p.dz, b, t0, vt, k, nk, out);
             }
-            store_token<S::kVec, RAGGED>(p.ddt, b, t0, vt, k, nk, out);
+#pragma unroll
+            for (int i = 0; i < V; i++) {
+                const float2 sums = steps[vt][vk + i];
+                out[i] = fmaf(skip[vk + i], G[i], sums.x * sums.y);
+                dd[i] = fmaf(G[i], (float)u[i], dd[i]);
+            }
+            store_token<V, RAGGED>(p.du, b, t0, vt, k, nk, out);
+#pragma unroll
+            for (int i = 0; i < V; i++) {
+                out[i] = fmaf((float)u[i], steps[vt][vk + i].y, grad[vt][vk + i] * kLn2) * sigmoid_of((float)dt[i] + bias[vk + i]);
+                dbias[i] += out[i];
+            }
+            store_token<V, RAGGED>(p.ddt, b, t0, vt, k, nk, out);
         }
         __syncthreads();
     }
@@ -253,21 +258,13 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
         }
     }
     if constexpr (!CARRY_ONLY) {
-        static_assert(S::kAcross == 4, "lanes of the same remainder by 4 hold the same channels");
-        float dd[S::kVec], dbias[S::kVec];
+        static_assert(S::kAcross == 8, "lanes of the same remainder by 8 hold the same channels");
 #pragma unroll
-        for (int i = 0; i < S::kVec; i++) {
-            dd[i] = add_dpp<0x128>(add_dpp<0x124>(over_tokens[0][i / 4][lane][i % 4]));
-            dd[i] += __shfl_xor(dd[i], 16, 64);
-            dd[i] += __shfl_xor(dd[i], 32, 64);
-            dbias[i] = add_dpp<0x128>(add_dpp<0x124>(over_tokens[1][i / 4][lane][i % 4]));
-            dbias[i] += __shfl_xor(dbias[i], 16, 64);
-            dbias[i] += __shfl_xor(dbias[i], 32, 64);
+        for (int i = 0; i < V; i++) {
+            const float half = sum_halves(add_dpp<0x128>(dd[i]), add_dpp<0x128>(dbias[i]));  // lanes 0 - 31: dd, 32 - 63: ddt_bias
+            dd[i] = sum_rows(half, half);
         }
-        if (lane < 4 && nk) {
-            store_first<S::kVec>(sums + (int64_t)p.K * p.N + k, nk, dd);
-            store_first<S::kVec>(sums + (int64_t)p.K * (p.N + 1) + k, nk, dbias);
-        }
+        if ((lane & 24) == 0 && nk) store_first<V>(sums + (int64_t)p.K * (p.N + (lane >> 5)) + k, nk, dd);
     }
 }
 

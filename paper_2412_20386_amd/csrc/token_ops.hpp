@@ -97,6 +97,18 @@ __device__ __forceinline__ float quad_sums(const float (&v)[C], int q) {
     const float mine = q & 1 ? v[C - 1] : v[0], other = q & 1 ? v[0] : v[C - 1];
     return add_dpp<0x4E>(mine + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, other), 0xB1, 0xf, 0xf, true)));
 }
+// Two values of each lane summed over pairs of lanes, one to a lane: lanes 0-31 get a's sums over lanes l and l + 32, lanes 32-63
+// b's; or rows of 16 lanes, the even rows a's over rows r and r + 1, the odd rows b's.  A swap and an addition for two sums.
+__device__ __forceinline__ float sum_halves(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ __forceinline__ float sum_rows(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+// Sum over the four lanes of a row of 16 that have the same place in their quads
+__device__ __forceinline__ float sum_quads(float v) { return add_dpp<0x128>(add_dpp<0x124>(v)); }  // row_ror 4, 8
 // Sum over an aligned group of `lanes` = 2^n lanes, in every lane of it
 __device__ __forceinline__ float group_sum(float v, int lanes) {
     if (lanes >= 2) v = add_dpp<0xB1>(v);    // quad_perm 1,0,3,2
