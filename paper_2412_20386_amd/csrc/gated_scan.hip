@@ -5,8 +5,8 @@ namespace {
 
 using namespace ptq4vm;
 
-constexpr int kTile = 16;  // tokens that are staged together
-constexpr int kAhead = 8;  // chunks whose states are loaded together
+constexpr int kTile = 16;           // tokens that are staged together
+constexpr int64_t kFull = 4096;     // wavefronts from which two channels to a lane are faster: 4 to a SIMD (3072: 112 us against 102)
 
 // One wavefront: 16 C channels of one sequence through the tokens of one chunk.
 // STATES_ONLY: from a zero state, without outputs; leaves the chunk's end state and its sum of D, from which the chunks behind
@@ -35,18 +35,21 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
 #pragma unroll
         for (int i = 0; i < NS; i++) a2[c][i] *= kLog2e, h[c][i] = 0.0f;
         if constexpr (!STATES_ONLY) {
-            if (p.state) load_channel<NS, RAGGED>(p.state, (int64_t)b * p.K + kc + c, n0, p.N, mine, h[c]);
-            for (uint32_t i = 0; i < chunk; i += kAhead) {  // (the loads of kAhead chunks are in flight together)
-                float end[kAhead][NS], D[kAhead];
+            if (p.joined && chunk > 0)
+                load_channel<NS, RAGGED>(p.chunk_state, ((int64_t)(chunk - 1) * p.B + b) * p.K + kc + c, n0, p.N, mine, h[c]);
+            else if (p.state)
+                load_channel<NS, RAGGED>(p.state, (int64_t)b * p.K + kc + c, n0, p.N, mine, h[c]);
+            if (!p.joined && chunk > 0) {
+                float end[kJoin - 2][NS], D[kJoin - 2];
 #pragma unroll
-                for (int s = 0; s < kAhead; s++) {
-                    const int64_t channel = ((int64_t)min(i + s, chunk - 1) * p.B + b) * p.K + (mine ? kc + c : 0);
+                for (int s = 0; s < kJoin - 2; s++) {
+                    const int64_t channel = ((int64_t)min((uint32_t)s, chunk - 1) * p.B + b) * p.K + (mine ? kc + c : 0);
                     load_channel<NS, RAGGED>(p.chunk_state, channel, n0, p.N, mine, end[s]);
                     D[s] = p.chunk_dt[channel];
                 }
 #pragma unroll
-                for (int s = 0; s < kAhead; s++)
-                    if (i + s < chunk)
+                for (int s = 0; s < kJoin - 2; s++)
+                    if ((uint32_t)s < chunk)
 #pragma unroll
                         for (int j = 0; j < NS; j++) h[c][j] = fmaf(__builtin_amdgcn_exp2f(a2[c][j] * D[s]), h[c][j], end[s][j]);
             }
@@ -208,7 +211,7 @@ extern "C" {
 
 int64_t ptq4vm_gated_scan_workspace(int64_t B, int64_t L, int64_t K, int64_t N) {
     if (!scan_sizes(B, L, K, N) || B == 0) return 0;
-    const ScanPlan plan = scan_plan(B, L, K, N);
+    const ScanPlan plan = scan_plan(B, L, K, N, kFull);
     return plan.chunks > 1 ? plan.chunks * B * K * (N + 1) * 4 : 0;
 }
 
@@ -222,7 +225,7 @@ int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, 
     if (workspace_bytes < need) return PTQ4VM_ERR_SHAPE;
     if (!aligned_to(state, 4) || !aligned_to(state_out, 4) || !aligned_to(marks, 4) || (need > 0 && !aligned_to(workspace, 16))) return PTQ4VM_ERR_ALIGN;
     if (B == 0) return PTQ4VM_OK;
-    const ScanPlan plan = scan_plan(B, L, K, N);
+    const ScanPlan plan = scan_plan(B, L, K, N, kFull);
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     return for_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
@@ -232,12 +235,15 @@ int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, 
         s.column_blocks = (int)plan.column_blocks, s.chunk_tokens = plan.chunk_tokens;
         return for_layout(plan, K, N, [&](auto ns, auto ch, auto ragged) {
             const auto go = [&](auto states_only, int64_t chunks) {
-                s.chunks = (uint32_t)chunks, s.blocks = (uint32_t)(chunks * B * plan.column_blocks);
+                s.blocks = (uint32_t)(chunks * B * plan.column_blocks);
                 gated_scan_tokens<T, ns(), ch(), ragged(), states_only()><<<dim3(xcd_grid(s.blocks)), dim3(64), 0, stream>>>(s);
                 return check_launch("gated_scan_tokens");
             };
             if (plan.chunks > 1)  // (nobody asks for the last chunk's)
                 if (const int e = go(std::true_type{}, plan.chunks - 1)) return e;
+            s.chunks = (uint32_t)plan.chunks, s.joined = plan.chunks >= kJoin;
+            if (s.joined)
+                if (const int e = launch_join_chunks<false>(s, stream)) return e;
             return go(std::false_type{}, plan.chunks);
         });
     });

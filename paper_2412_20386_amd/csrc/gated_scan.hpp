@@ -28,6 +28,7 @@ struct ScanArgs {
     int B, K, N, column_blocks;
     int64_t L, chunk_tokens;  // (a multiple of 16)
     uint32_t chunks, blocks;
+    bool joined;  // chunk_state holds what comes into the next chunk, not what each leaves by itself
 };
 
 // What the layout of a wavefront makes of its lane number, where TOKENS tokens are staged at once
@@ -42,23 +43,24 @@ struct ScanLane {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// Channels and states of the kernels' variants: states in quads of 1, 4 or 16 each, two channels to a lane where that leaves
-// two wavefronts to a SIMD
+// States of a quad's lane: 1, 4 or 16
 inline int states_per_lane(int64_t N) { return N <= 4 ? 1 : N <= 16 ? 4 : 16; }
-inline int channels_per_lane(int64_t B, int64_t K, int64_t N) { return N <= 16 && B * ceil_div(K, 32) >= 2048 ? 2 : 1; }
 
-// Chunks of a sequence: one unless that leaves the device half empty, then as many as fill it, of two tiles at least
+// How a problem is cut: two channels to a lane where that leaves `full` wavefronts, and one chunk of tokens per sequence unless
+// the device would be half empty; then chunks for 4096 wavefronts, of 32 tokens at least.
+// From kJoin chunks on, a kernel of its own runs through them; up to there each wavefront does, all loads in flight.
+constexpr int kMostChunks = 128, kJoin = 9;
 struct ScanPlan {
     int channels, states;
     int64_t column_blocks, chunk_tokens, chunks;
 };
-inline ScanPlan scan_plan(int64_t B, int64_t L, int64_t K, int64_t N) {
-    ScanPlan p{channels_per_lane(B, K, N), states_per_lane(N), 0, 0, 0};
+inline ScanPlan scan_plan(int64_t B, int64_t L, int64_t K, int64_t N, int64_t full) {
+    ScanPlan p{N <= 16 && B * ceil_div(K, 32) >= full ? 2 : 1, states_per_lane(N), 0, 0, 0};
     p.column_blocks = ceil_div(K, 16 * p.channels);
     const int64_t waves = B * p.column_blocks;
     int64_t chunks = waves >= 1024 ? 1 : ceil_div(4096, waves > 0 ? waves : 1);
     if (chunks > ceil_div(L, 32)) chunks = ceil_div(L, 32);
-    if (chunks > 128) chunks = 128;
+    if (chunks > kMostChunks) chunks = kMostChunks;
     p.chunk_tokens = ceil_div(ceil_div(L, chunks), 16) * 16;
     p.chunks = ceil_div(L, p.chunk_tokens);
     return p;
@@ -140,5 +142,56 @@ __device__ __forceinline__ void store_channel(float *p, int64_t channel, int n0,
         store_first<NS>(p + channel * (4 * NS) + n0, NS, v);
     }
 }
+
+namespace {
+
+// Runs through the chunks of a sequence for every state.  A chunk's slot i holds what it leaves by itself, end(i), and its sum of D;
+// in(i + 1) = exp(a sum D(i)) in(i) + end(i) replaces end(i) (the first chunk's in is the state, or 0).  BACKWARD: the same from
+// the last chunk to the first.  16 lanes take adjacent states, 16 of those groups a run of chunks each: a run's values are
+// loaded at once, the runs are joined through LDS, and then the run writes what comes into its chunks.
+constexpr int kJoinStates = 16, kJoinRuns = 16, kJoinRun = kMostChunks / kJoinRuns;
+template <bool BACKWARD>
+__global__ __launch_bounds__(kJoinStates *kJoinRuns) void join_chunks(float *__restrict__ chunk_state, const float *__restrict__ chunk_dt, const float *__restrict__ a,
+                                                                     const float *__restrict__ state, int64_t channels, int K, int N, int chunks) {
+    __shared__ float ends[kJoinRuns][kJoinStates], sums[kJoinRuns][kJoinStates];
+    const int s = threadIdx.x % kJoinStates, run = threadIdx.x / kJoinStates;
+    const int64_t at = (int64_t)blockIdx.x * kJoinStates + s;
+    const bool there = at < channels * N;
+    const int64_t channel = there ? at / N : 0;
+    const int steps = chunks - 1;                                    // chunks that leave something to another one
+    const int length = (steps + kJoinRuns - 1) / kJoinRuns, first = run * length;
+    const float a2 = there ? a[channel % K * N + (at - channel * N)] * kLog2e : 0.0f;
+    float end[kJoinRun], D[kJoinRun], h = 0.0f, sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kJoinRun; i++) {
+        const bool mine = there && i < length && first + i < steps;
+        const int64_t slot = BACKWARD ? chunks - 1 - (first + i) : first + i;
+        end[i] = mine ? chunk_state[slot * channels * N + at] : 0.0f;
+        D[i] = mine ? chunk_dt[slot * channels + channel] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kJoinRun; i++) {
+        h = fmaf(__builtin_amdgcn_exp2f(a2 * D[i]), h, end[i]);
+        sum += D[i];
+    }
+    ends[run][s] = h, sums[run][s] = sum;
+    __syncthreads();
+    h = !BACKWARD && state && there ? state[at] : 0.0f;
+    for (int r = 0; r < run; r++) h = fmaf(__builtin_amdgcn_exp2f(a2 * sums[r][s]), h, ends[r][s]);
+#pragma unroll
+    for (int i = 0; i < kJoinRun; i++) {
+        h = fmaf(__builtin_amdgcn_exp2f(a2 * D[i]), h, end[i]);
+        if (there && i < length && first + i < steps) chunk_state[(BACKWARD ? chunks - 1 - (first + i) : first + i) * channels * N + at] = h;
+    }
+}
+template <bool BACKWARD, typename T>
+int launch_join_chunks(const ScanArgs<T> &s, hipStream_t stream) {
+    const int64_t channels = (int64_t)s.B * s.K;
+    join_chunks<BACKWARD><<<dim3((unsigned)ceil_div(channels * s.N, kJoinStates)), dim3(kJoinStates * kJoinRuns), 0, stream>>>(
+        s.chunk_state, s.chunk_dt, s.a, s.state, channels, s.K, s.N, (int)s.chunks);
+    return check_launch("join_chunks");
+}
+
+}  // namespace
 
 }  // namespace ptq4vm

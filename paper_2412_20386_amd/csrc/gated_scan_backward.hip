@@ -14,13 +14,13 @@ namespace {
 using namespace ptq4vm;
 
 constexpr int kTile = kMark;  // tokens that are staged together, and whose states are in registers
-constexpr int kAhead = 8;  // chunks whose carries are loaded together
+constexpr int64_t kFull = 2048;  // wavefronts from which two channels to a lane are faster: 2 to a SIMD (3072: 275 us against 295)
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // CARRY_ONLY: from a zero gradient behind the chunk, without outputs; leaves e^{D a} g at the chunk's first token and the sum
 // of D, from which the chunks before it know the gradient that comes in.
 template <typename T, int NS, int C, bool RAGGED, bool CARRY_ONLY>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 1 : CARRY_ONLY ? 4 : 2))) void gated_scan_backward_tokens(ScanArgs<T> p) {
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 1 : CARRY_ONLY ? 4 : C == 1 ? 3 : 2))) void gated_scan_backward_tokens(ScanArgs<T> p) {
     using S = ScanLane<NS, C, kTile>;
     constexpr int V = S::kVec;
     alignas(16) __shared__ float2 steps[kTile][S::kChannels];  // D and D u, then sum g b
@@ -45,22 +45,24 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
         sum_d[c] = 0.0f;
 #pragma unroll
         for (int i = 0; i < NS; i++) a2[c][i] *= kLog2e, carry[c][i] = da[c][i] = 0.0f;
-        if constexpr (!CARRY_ONLY)
-            for (uint32_t i = p.chunks - 1; i > chunk; i -= min(i, (uint32_t)kAhead)) {
-                float end[kAhead][NS], D[kAhead];
+        if constexpr (!CARRY_ONLY) {
+            if (p.joined) {
+                if (chunk + 1 < p.chunks) load_channel<NS, RAGGED>(p.chunk_state, ((int64_t)(chunk + 1) * p.B + b) * p.K + kc + c, n0, p.N, mine, carry[c]);
+            } else if (chunk + 1 < p.chunks) {
+                float end[kJoin - 2][NS], D[kJoin - 2];
 #pragma unroll
-                for (int s = 0; s < kAhead; s++) {
-                    const uint32_t from = i > chunk + s ? i - s : chunk + 1;
-                    const int64_t channel = ((int64_t)from * p.B + b) * p.K + (mine ? kc + c : 0);
+                for (int s = 0; s < kJoin - 2; s++) {  // from the last chunk on
+                    const int64_t channel = ((int64_t)max((int)p.chunks - 1 - s, (int)chunk + 1) * p.B + b) * p.K + (mine ? kc + c : 0);
                     load_channel<NS, RAGGED>(p.chunk_state, channel, n0, p.N, mine, end[s]);
                     D[s] = p.chunk_dt[channel];
                 }
 #pragma unroll
-                for (int s = 0; s < kAhead; s++)
-                    if (i > chunk + s)
+                for (int s = 0; s < kJoin - 2; s++)
+                    if ((int)p.chunks - 1 - s > (int)chunk)
 #pragma unroll
                         for (int j = 0; j < NS; j++) carry[c][j] = fmaf(__builtin_amdgcn_exp2f(a2[c][j] * D[s]), carry[c][j], end[s][j]);
             }
+        }
     }
 
     // what this lane loads: V channels of a token
@@ -304,7 +306,7 @@ extern "C" {
 
 int64_t ptq4vm_gated_scan_backward_workspace(int64_t B, int64_t L, int64_t K, int64_t N) {
     if (!scan_sizes(B, L, K, N) || B == 0) return 0;
-    const BackwardSizes s = backward_sizes(scan_plan(B, L, K, N), B, L, K, N);
+    const BackwardSizes s = backward_sizes(scan_plan(B, L, K, N, kFull), B, L, K, N);
     return (s.bc + s.a + s.chunk) * 4;
 }
 
@@ -333,7 +335,7 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     const SumOut parameters{da, dd, ddt_bias, K * N, K};
     if (B == 0) return launch_sum_partials(nullptr, 0, K * (N + 2), parameters, stream);
-    const ScanPlan plan = scan_plan(B, L, K, N);
+    const ScanPlan plan = scan_plan(B, L, K, N, kFull);
     const BackwardSizes sizes = backward_sizes(plan, B, L, K, N);
     float *const ws = static_cast<float *>(workspace);
     const int64_t values = B * L * 2 * N;
@@ -356,6 +358,9 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
             };
             if (plan.chunks > 1)
                 if (const int e3 = go(std::true_type{}, plan.chunks - 1)) return e3;
+            s.joined = plan.chunks >= kJoin;
+            if (s.joined)
+                if (const int e3 = launch_join_chunks<true>(s, stream)) return e3;
             return go(std::false_type{}, plan.chunks);
         });
         if (e2) return e2;
