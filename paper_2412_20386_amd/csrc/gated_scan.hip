@@ -144,40 +144,33 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
 }
 
 // One token of every sequence: bound by the states, which are read and written once (128 bytes of a channel's 16 against 10
-// of everything else).  A quad of lanes takes a channel, its lanes adjacent states.  A lane's states are read before they are
-// written by it alone, so state_out may be the state's own buffer.
-template <typename T, int NS>
+// of everything else).  A quad of lanes takes a channel, its lanes adjacent states; a workgroup 64 channels of one sequence.  A
+// lane's states are read before they are written by it alone, so state_out may be the state's own buffer.
+template <typename T, int NS, bool RAGGED>
 __global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
-    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 2;
-    const int q = threadIdx.x & 3, n0 = q * NS;
-    const bool there = at < (int64_t)p.B * p.K;
-    const int64_t ch = there ? at : 0;
-    const int b = (int)(ch / p.K), k = (int)(ch - (int64_t)b * p.K);
+    const int b = blockIdx.x / p.column_blocks, k = (int)(blockIdx.x - b * p.column_blocks) * 64 + (threadIdx.x >> 2);
+    const int q = threadIdx.x & 3, n0 = q * NS, n = RAGGED ? max(0, min(NS, p.N - n0)) : NS;
+    if (k >= p.K) return;  // (whole quads)
     float h[NS], a[NS];
     T B[NS], CC[NS];
-    const int n = max(0, min(NS, p.N - n0));
-    load_channel<NS, true>(p.state, ch, n0, p.N, true, h);
-    load_channel<NS, true>(p.a, k, n0, p.N, true, a);
+    load_channel<NS, RAGGED>(p.state, (int64_t)b * p.K + k, n0, p.N, true, h);
+    load_channel<NS, RAGGED>(p.a, k, n0, p.N, true, a);
     load_first<NS>(p.b.at(b, 0) + n0, n, B);
     load_first<NS>(p.c.at(b, 0) + n0, n, CC);
     const float u = (float)p.u.at(b, 0)[k];
     const float D = softplus_of((float)p.dt.at(b, 0)[k] + (p.dt_bias ? p.dt_bias[k] : 0.0f)), Du = D * u;
+    const float z = p.z.data ? (float)p.z.at(b, 0)[k] : 0.0f;
     float v = 0.0f;
 #pragma unroll
     for (int i = 0; i < NS; i++) {
         h[i] = fmaf(__builtin_amdgcn_exp2f(a[i] * kLog2e * D), h[i], Du * (float)B[i]);
         v = i < n ? fmaf(h[i], (float)CC[i], v) : v;
     }
+    store_channel<NS, RAGGED>(p.state_out, (int64_t)b * p.K + k, n0, p.N, true, h);
     v = quad_sum(v);
-    if (!there) return;
-    store_channel<NS, true>(p.state_out, ch, n0, p.N, true, h);
-    if (q != 0) return;
     if (p.d) v = fmaf(p.d[k], u, v);
-    if (p.z.data) {
-        const float z = (float)p.z.at(b, 0)[k];
-        v *= z * sigmoid_of(z);
-    }
-    p.y.at(b, 0)[k] = (T)v;
+    if (p.z.data) v *= z * sigmoid_of(z);
+    if (q == 0) p.y.at(b, 0)[k] = (T)v;
 }
 
 int check_scan(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d, const void *z, const float *dt_bias, void *y,
@@ -257,20 +250,23 @@ int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float
     if (B != 0 && (!state || !state_out)) return PTQ4VM_ERR_NULL;
     if (!aligned_to(state, 4) || !aligned_to(state_out, 4)) return PTQ4VM_ERR_ALIGN;
     if (B == 0) return PTQ4VM_OK;
-    const int64_t blocks = ceil_div(B * K, 64);
-    if (blocks > kMaxTokenRows) return PTQ4VM_ERR_SHAPE;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     return for_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
         ScanArgs<T> s = scan_args<T>(u, dt, a, b, c, d, z, dt_bias, y, false, B, 1, K, N, ldu, lddt, ldb, ldc, ldz, ldy);
         s.state = state, s.state_out = state_out;
-        const dim3 grid((unsigned)blocks);
+        s.column_blocks = (int)ceil_div(K, 64);
+        using std::integral_constant;
+        const auto go = [&](auto ns, auto ragged) {
+            gated_scan_one_token<T, ns(), ragged()><<<dim3((unsigned)(B * s.column_blocks)), dim3(256), 0, stream>>>(s);
+            return check_launch("gated_scan_one_token");
+        };
+        const auto with = [&](auto ns) { return N == 4 * ns() ? go(ns, std::false_type{}) : go(ns, std::true_type{}); };
         switch (states_per_lane(N)) {
-            case 1: gated_scan_one_token<T, 1><<<grid, dim3(256), 0, stream>>>(s); break;
-            case 4: gated_scan_one_token<T, 4><<<grid, dim3(256), 0, stream>>>(s); break;
-            default: gated_scan_one_token<T, 16><<<grid, dim3(256), 0, stream>>>(s); break;
+            case 1: return with(integral_constant<int, 1>{});
+            case 4: return with(integral_constant<int, 4>{});
+            default: return with(integral_constant<int, 16>{});
         }
-        return check_launch("gated_scan_one_token");
     });
 }
 
