@@ -115,8 +115,8 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
     if (lanes >= 4) v = add_dpp<0x4E>(v);    // quad_perm 2,3,0,1
     if (lanes >= 8) v = add_dpp<0x141>(v);   // row_half_mirror: quads of 8 lanes
     if (lanes >= 16) v = add_dpp<0x140>(v);  // row_mirror: halves of 16 lanes
-    if (lanes >= 32) v += __shfl_xor(v, 16, 64);
-    if (lanes >= 64) v += __shfl_xor(v, 32, 64);
+    if (lanes >= 32) v = sum_rows(v, v);
+    if (lanes >= 64) v = sum_halves(v, v);
     return v;
 }
 
@@ -126,20 +126,20 @@ struct SumOut {
     float *out0, *out1, *out2;
     int64_t first, second;
 };
-constexpr int kSumThreads = 256, kSumCols = 32;
+constexpr int kSumThreads = 1024, kSumCols = 32;  // (32 rows at a time: sums of 1024 rows take 32 round trips to memory)
 namespace {
-__global__ __launch_bounds__(kSumThreads) void sum_partials(const float *__restrict__ partial, int64_t rows, int64_t cols, SumOut out) {
+__device__ __forceinline__ void sum_columns(const float *__restrict__ partial, int64_t rows, int64_t stride, int64_t cols, const SumOut &out, uint32_t block) {
     constexpr int kSlots = kSumThreads / kSumCols;
     __shared__ float red[kSlots][kSumCols];
     const int slot = threadIdx.x / kSumCols, c = threadIdx.x % kSumCols;
-    const int64_t col = (int64_t)blockIdx.x * kSumCols + c;
+    const int64_t col = (int64_t)block * kSumCols + c;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (col < cols) {
         int64_t r = slot;
         for (; r + 3 * kSlots < rows; r += 4 * kSlots)
 #pragma unroll
-            for (int i = 0; i < 4; i++) sum[i] += partial[(r + i * kSlots) * cols + col];
-        for (; r < rows; r += kSlots) sum[0] += partial[r * cols + col];
+            for (int i = 0; i < 4; i++) sum[i] += partial[(r + i * kSlots) * stride + col];
+        for (; r < rows; r += kSlots) sum[0] += partial[r * stride + col];
     }
     red[slot][c] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     __syncthreads();
@@ -147,9 +147,13 @@ __global__ __launch_bounds__(kSumThreads) void sum_partials(const float *__restr
         float v = 0.0f;
 #pragma unroll
         for (int i = 0; i < kSlots; i++) v += red[i][c];
-        float *const to = col < out.first ? out.out0 + col : col < out.first + out.second ? out.out1 + (col - out.first) : out.out2 + (col - out.first - out.second);
-        if ((col < out.first ? out.out0 : col < out.first + out.second ? out.out1 : out.out2) != nullptr) *to = v;
+        float *const to = col < out.first ? out.out0 : col < out.first + out.second ? out.out1 : out.out2;
+        const int64_t at = col < out.first ? col : col < out.first + out.second ? col - out.first : col - out.first - out.second;
+        if (to) to[at] = v;
     }
+}
+__global__ __launch_bounds__(kSumThreads) void sum_partials(const float *__restrict__ partial, int64_t rows, int64_t cols, SumOut out) {
+    sum_columns(partial, rows, cols, cols, out, blockIdx.x);
 }
 inline int launch_sum_partials(const float *partial, int64_t rows, int64_t cols, const SumOut &out, hipStream_t stream) {
     sum_partials<<<dim3((unsigned)ceil_div(cols, kSumCols)), dim3(kSumThreads), 0, stream>>>(partial, rows, cols, out);
