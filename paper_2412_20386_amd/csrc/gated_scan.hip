@@ -216,7 +216,7 @@ int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, 
     const int64_t need = ptq4vm_gated_scan_workspace(B, L, K, N);
     if (need > 0 && !workspace) return PTQ4VM_ERR_NULL;
     if (workspace_bytes < need) return PTQ4VM_ERR_SHAPE;
-    if (!aligned_to(state, 4) || !aligned_to(state_out, 4) || !aligned_to(marks, 4) || (need > 0 && !aligned_to(workspace, 16))) return PTQ4VM_ERR_ALIGN;
+    if (!aligned_to(state, 4) || !aligned_to(state_out, 4) || !aligned_to(marks, 4) || !aligned_to(workspace, 16)) return PTQ4VM_ERR_ALIGN;
     if (B == 0) return PTQ4VM_OK;
     const ScanPlan plan = scan_plan(B, L, K, N, kFull);
     hipStream_t stream = static_cast<hipStream_t>(stream_);

@@ -331,7 +331,7 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
         if (!aligned_to(ptr, e)) return PTQ4VM_ERR_ALIGN;
     for (const void *ptr : {(const void *)a, (const void *)d, (const void *)dt_bias, (const void *)marks, (const void *)da, (const void *)dd, (const void *)ddt_bias})
         if (!aligned_to(ptr, 4)) return PTQ4VM_ERR_ALIGN;
-    if (need > 0 && !aligned_to(workspace, 16)) return PTQ4VM_ERR_ALIGN;
+    if (!aligned_to(workspace, 16)) return PTQ4VM_ERR_ALIGN;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     const SumOut parameters{da, dd, ddt_bias, K * N, K};
     if (B == 0) return launch_sum_partials(nullptr, 0, K * (N + 2), parameters, stream);

@@ -463,6 +463,9 @@ float real(PyObject *o, double otherwise) {
     if (v == -1.0 && PyErr_Occurred()) throw Raised{};
     return (float)v;
 }
+void rows_of_sequences(int64_t M, int64_t B, int64_t L, const char *name) {
+    if (B < 0 || L <= 0 || !is_product(M, B, L)) raise(PyExc_ValueError, std::string(name) + " must have B*L rows");
+}
 void *scratch_data(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
 int64_t scratch_bytes(const at::Tensor &t) { return t.defined() ? t.numel() : 0; }
 void not_the_same(const void *a, const void *b, const char *name) {
@@ -513,7 +516,7 @@ PyObject *gated_scan(Args a) {  // u dt a b c d z dt_bias B L reverse state y st
     const Operands ops(a[0], "u");
     const ScanInputs in(ops, a);
     const int64_t B = integer(a[8]), L = integer(a[9]), K = in.K, N = in.N;
-    if (!is_product(in.u.rows, B, L)) raise(PyExc_ValueError, "u must have B*L rows");
+    rows_of_sequences(in.u.rows, B, L, "u");
     const bool reverse = truth(a[10], false);
     const float *state = floats(ops.dense_or_null(a[11], at::kFloat, {B, K, N}, "state"));
     Owned out(output(a[12], {in.u.rows, K}, ops.dtype, a[0]));
@@ -531,9 +534,8 @@ PyObject *gated_scan_backward(Args a) {  // dy u dt a b c d z dt_bias marks B L 
     const Operands ops(a[1], "u");
     const ScanInputs in(ops, a + 1);
     const int64_t B = integer(a[10]), L = integer(a[11]), M = in.u.rows, K = in.K, N = in.N;
-    if (!is_product(M, B, L)) raise(PyExc_ValueError, "u must have B*L rows");
+    rows_of_sequences(M, B, L, "u");
     const Matrix dy = ops.in(a[0], M, K, "dy");
-    if (L <= 0) raise(PyExc_ValueError, "L must be positive");
     const float *marks = floats(ops.dense(a[9], at::kFloat, {PTQ4VM_SCAN_MARKS(L), B, K, N}, "marks"));
     const bool reverse = truth(a[12], false);
     if (given(a[17]) && !in.z.data && !given(a[7])) raise(PyExc_ValueError, "dz: there is no z");
@@ -583,7 +585,7 @@ PyObject *token_conv(Args a) {  // x w bias B L silu reverse state y state_out
     const Operands ops(a[0], "x");
     const ConvInputs in(ops, a);
     const int64_t B = integer(a[3]), L = integer(a[4]), K = in.K, W = in.W;
-    same_rows(in.x.rows, B, L);
+    rows_of_sequences(in.x.rows, B, L, "x");
     const bool silu = truth(a[5], true), reverse = truth(a[6], false);
     const void *state = ops.dense_or_null(a[7], ops.dtype, {B, W - 1, K}, "state");
     Owned out(output(a[8], {in.x.rows, K}, ops.dtype, a[0]));
@@ -598,7 +600,7 @@ PyObject *token_conv_backward(Args a) {  // dy x w bias B L silu reverse state d
     const Operands ops(a[1], "x");
     const ConvInputs in(ops, a + 1);
     const int64_t B = integer(a[4]), L = integer(a[5]), M = in.x.rows, K = in.K, W = in.W;
-    same_rows(M, B, L);
+    rows_of_sequences(M, B, L, "x");
     const Matrix dy = ops.in(a[0], M, K, "dy");
     const bool silu = truth(a[6], true), reverse = truth(a[7], false);
     const void *state = ops.dense_or_null(a[8], ops.dtype, {B, W - 1, K}, "state");
