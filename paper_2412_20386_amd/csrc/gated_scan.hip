@@ -143,6 +143,78 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
         }
 }
 
+// Few short sequences of few channels, up to 16 states: a lane takes one state, a wavefront 4 channels of one tile of tokens, a
+// workgroup all tiles of a sequence.  The tiles run side by side from a zero state, tell each other through LDS what they leave and
+// their sums of D, and run again from their true first states on what is staged already: one launch, and of the tokens'
+// latencies those of two tiles, on four times the compute units that quads of lanes would fill (sums over 16 lanes cost four
+// additions a token for it).  One image, 197 tokens x 384 channels x 16 states: 12 us in chunks (two launches), 10.8 us with quads of
+// lanes here, and 6.0 us so.
+constexpr int kShortTiles = 16, kShortStates = 16, kShortChannels = 4;
+template <typename T, bool RAGGED>
+__global__ __launch_bounds__(kShortTiles * 64) void gated_scan_short(ScanArgs<T> p) {
+    struct Tile {
+        float2 steps[kTile][kShortChannels];  // D and D u; then s without its d u in D's place
+        float b[kTile][kShortStates], c[kTile][kShortStates];
+        float end[kShortChannels][kShortStates], sum_d[kShortChannels];
+    };
+    alignas(16) __shared__ Tile tiles[kShortTiles];
+    const uint32_t block = xcd_contiguous(blockIdx.x, p.blocks);
+    if (block >= p.blocks) return;
+    const int cb = block % p.column_blocks, b = block / p.column_blocks, lane = threadIdx.x & 63;
+    Tile &tile = tiles[threadIdx.x >> 6];
+    const int64_t t0 = (int64_t)(threadIdx.x >> 6) * kTile;
+    const int last = (int)min((int64_t)kTile, p.L - t0) - 1;
+    // what the lane loads: one channel of a token, four states of a token's b and c
+    const int vt = lane >> 2, vc = lane & 3, k = cb * kShortChannels + vc, from = min(vt, last);
+    const bool column = !RAGGED || k < p.K;
+    const float x = column ? (float)*in_tile(p.dt, b, t0, from, k) : 0.0f, u = column ? (float)*in_tile(p.u, b, t0, from, k) : 0.0f;
+    const float z = column && p.z.data ? (float)*in_tile(p.z, b, t0, from, k) : 0.0f;
+    T rb[4], rc[4];
+    const int n_load = RAGGED ? max(0, min(4, p.N - vc * 4)) : 4;
+    load_first<4>(in_tile(p.b, b, t0, from, vc * 4), n_load, rb);
+    load_first<4>(in_tile(p.c, b, t0, from, vc * 4), n_load, rc);
+    const float bias = column && p.dt_bias ? p.dt_bias[k] : 0.0f, skip = column && p.d ? p.d[k] : 0.0f;
+    // what it runs: one state
+    const int n = lane & 15, cl = lane >> 4, kc = cb * kShortChannels + cl;
+    const bool mine = !RAGGED || (kc < p.K && n < p.N);
+    const int64_t state = (int64_t)kc * p.N + n;
+    const float a2 = mine ? p.a[state] * kLog2e : 0.0f;
+    const float start = mine && p.state ? p.state[(int64_t)b * p.K * p.N + state] : 0.0f;
+
+    const float D_in = softplus_of(x + bias);
+    tile.steps[vt][vc] = {vt <= last ? D_in : 0.0f, vt <= last ? D_in * u : 0.0f};  // (tokens behind the last change nothing)
+#pragma unroll
+    for (int i = 0; i < 4; i++) tile.b[vt][vc * 4 + i] = vt <= last ? (float)rb[i] : 0.0f, tile.c[vt][vc * 4 + i] = (float)rc[i];
+    __syncthreads();
+    float h = 0.0f, sum = 0.0f;
+    const auto advance = [&](int t) {
+        const float2 D = tile.steps[t][cl];
+        h = fmaf(__builtin_amdgcn_exp2f(a2 * D.x), h, D.y * tile.b[t][n]);
+        if (RAGGED) h = mine ? h : 0.0f;
+        return D.x;
+    };
+#pragma unroll
+    for (int t = 0; t < kTile; t++) sum += advance(t);
+    tile.end[cl][n] = h;
+    if (n == 0) tile.sum_d[cl] = sum;
+    __syncthreads();
+    h = start;
+    for (int s = 0; s < (int)(threadIdx.x >> 6); s++) h = fmaf(__builtin_amdgcn_exp2f(a2 * tiles[s].sum_d[cl]), h, tiles[s].end[cl][n]);
+#pragma unroll
+    for (int t = 0; t < kTile; t++) {
+        if (p.marks && t % kMark == 0 && t <= last && mine) p.marks[((t0 + t) / kMark * p.B + b) * p.K * p.N + state] = h;
+        advance(t);
+        tile.steps[t][cl].x = group_sum(RAGGED && n >= p.N ? 0.0f : h * tile.c[t][n], 16);  // (the lanes' reads of D are done: one wavefront, LDS in order)
+    }
+    __syncthreads();
+    if (vt <= last && column) {
+        float y = fmaf(skip, u, tile.steps[vt][vc].x);
+        if (p.z.data) y *= z * sigmoid_of(z);
+        *in_tile(p.y, b, t0, vt, k) = (T)y;
+    }
+    if (p.state_out && t0 + last + 1 == p.L && mine) p.state_out[(int64_t)b * p.K * p.N + state] = h;
+}
+
 // One token of every sequence: bound by the states, which are read and written once (128 bytes of a channel's 16 against 10
 // of everything else).  A quad of lanes takes a channel, its lanes adjacent states; a workgroup 64 channels of one sequence.  A
 // lane's states are read before they are written by it alone, so state_out may be the state's own buffer.
@@ -171,6 +243,12 @@ __global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
     if (p.d) v = fmaf(p.d[k], u, v);
     if (p.z.data) v *= z * sigmoid_of(z);
     if (q == 0) p.y.at(b, 0)[k] = (T)v;
+}
+
+// Whether the tiles of a sequence run side by side in one workgroup: up to three workgroups on a compute unit (197 tokens x 1536
+// channels, us against chunks or one wavefront a sequence: 1 image 8.1 / 12.0, 2 images 11.9 / 15.2, 3 images 18.5 / 16.7)
+bool is_short(int64_t B, int64_t L, int64_t K, int64_t N) {
+    return N <= kShortStates && L > kTile && L <= kShortTiles * kTile && B * ceil_div(K, kShortChannels) <= 768;
 }
 
 int check_scan(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d, const void *z, const float *dt_bias, void *y,
@@ -205,7 +283,7 @@ extern "C" {
 int64_t ptq4vm_gated_scan_workspace(int64_t B, int64_t L, int64_t K, int64_t N) {
     if (!scan_sizes(B, L, K, N) || B == 0) return 0;
     const ScanPlan plan = scan_plan(B, L, K, N, kFull);
-    return plan.chunks > 1 ? plan.chunks * B * K * (N + 1) * 4 : 0;
+    return plan.chunks > 1 && !is_short(B, L, K, N) ? plan.chunks * B * K * (N + 1) * 4 : 0;
 }
 
 int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d, const void *z, const float *dt_bias,
@@ -226,6 +304,15 @@ int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, 
         s.state = state, s.state_out = state_out, s.marks = marks;
         s.chunk_state = static_cast<float *>(workspace), s.chunk_dt = s.chunk_state + (plan.chunks > 1 ? plan.chunks * B * K * N : 0);
         s.column_blocks = (int)plan.column_blocks, s.chunk_tokens = plan.chunk_tokens;
+        if (is_short(B, L, K, N)) {
+            s.column_blocks = (int)ceil_div(K, kShortChannels), s.blocks = (uint32_t)(B * s.column_blocks);
+            const dim3 grid(xcd_grid(s.blocks)), block((unsigned)ceil_div(L, kTile) * 64);
+            if (N == kShortStates && K % kShortChannels == 0)
+                gated_scan_short<T, false><<<grid, block, 0, stream>>>(s);
+            else
+                gated_scan_short<T, true><<<grid, block, 0, stream>>>(s);
+            return check_launch("gated_scan_short");
+        }
         return for_layout(plan, K, N, [&](auto ns, auto ch, auto ragged) {
             const auto go = [&](auto states_only, int64_t chunks) {
                 s.blocks = (uint32_t)(chunks * B * plan.column_blocks);
