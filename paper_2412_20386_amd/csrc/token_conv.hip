@@ -239,12 +239,14 @@ __global__ __launch_bounds__(kThreads) void token_conv_backward_runs(ConvArgs<T>
     }
 }
 
-// Lanes side by side over K, and the workgroups that K takes
+// Lanes side by side over K, and the workgroups that K takes: 64 lanes, fewer where that leaves fewer of them idle (768 channels
+// of 8 to a lane are 3 x 32)
 template <typename T>
 void columns(ConvArgs<T> &a, int64_t K, int vec) {
     const int64_t chunks = ceil_div(K, vec);
-    a.lanes_log2 = 0;
-    while ((1 << a.lanes_log2) < chunks && a.lanes_log2 < 6) a.lanes_log2++;
+    a.lanes_log2 = 6;
+    for (int lanes_log2 = 5; lanes_log2 >= 0; lanes_log2--)
+        if (ceil_div(chunks, 1 << lanes_log2) << lanes_log2 < ceil_div(chunks, 1 << a.lanes_log2) << a.lanes_log2 && (lanes_log2 >= 3 || chunks <= 4)) a.lanes_log2 = lanes_log2;
     a.column_blocks = (int)ceil_div(chunks, 1 << a.lanes_log2);
 }
 
