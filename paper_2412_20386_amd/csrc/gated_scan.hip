@@ -7,6 +7,7 @@ using namespace ptq4vm;
 
 constexpr int kTile = 16;           // tokens that are staged together
 constexpr int64_t kFull = 4096;     // wavefronts from which two channels to a lane are faster: 4 to a SIMD (3072: 112 us against 102)
+constexpr int64_t kHeld = 6144;     // wavefronts that sequences are cut for (16384 x 768: 2048 134 us, 4096 110, 5120 103, 6144 102)
 
 // One wavefront: 16 C channels of one sequence through the tokens of one chunk.
 // STATES_ONLY: from a zero state, without outputs; leaves the chunk's end state and its sum of D, from which the chunks behind
@@ -282,7 +283,7 @@ extern "C" {
 
 int64_t ptq4vm_gated_scan_workspace(int64_t B, int64_t L, int64_t K, int64_t N) {
     if (!scan_sizes(B, L, K, N) || B == 0) return 0;
-    const ScanPlan plan = scan_plan(B, L, K, N, kFull);
+    const ScanPlan plan = scan_plan(B, L, K, N, kFull, kHeld, kTile);
     return plan.chunks > 1 && !is_short(B, L, K, N) ? plan.chunks * B * K * (N + 1) * 4 : 0;
 }
 
@@ -296,7 +297,7 @@ int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, 
     if (workspace_bytes < need) return PTQ4VM_ERR_SHAPE;
     if (!aligned_to(state, 4) || !aligned_to(state_out, 4) || !aligned_to(marks, 4) || !aligned_to(workspace, 16)) return PTQ4VM_ERR_ALIGN;
     if (B == 0) return PTQ4VM_OK;
-    const ScanPlan plan = scan_plan(B, L, K, N, kFull);
+    const ScanPlan plan = scan_plan(B, L, K, N, kFull, kHeld, kTile);
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     return for_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
@@ -336,6 +337,7 @@ int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float
     if (rc != PTQ4VM_OK) return rc;
     if (B != 0 && (!state || !state_out)) return PTQ4VM_ERR_NULL;
     if (!aligned_to(state, 4) || !aligned_to(state_out, 4)) return PTQ4VM_ERR_ALIGN;
+    if (!grid_fits(B * ceil_div(K, 64), 256)) return PTQ4VM_ERR_SHAPE;
     if (B == 0) return PTQ4VM_OK;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     return for_dtype(dtype, [&](auto zero) {

@@ -26,7 +26,7 @@ struct ScanArgs {
     Tokens<T> dy, du, ddt, dz;
     float *partial_bc, *partial_a;
     int B, K, N, column_blocks;
-    int64_t L, chunk_tokens;  // (a multiple of 16)
+    int64_t L, chunk_tokens;  // (whole tiles)
     uint32_t chunks, blocks;
     bool joined;  // chunk_state holds what comes into the next chunk, not what each leaves by itself
 };
@@ -46,22 +46,21 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // States of a quad's lane: 1, 4 or 16
 inline int states_per_lane(int64_t N) { return N <= 4 ? 1 : N <= 16 ? 4 : 16; }
 
-// How a problem is cut: two channels to a lane where that leaves `full` wavefronts, and one chunk of tokens per sequence unless
-// the device would be half empty; then chunks for 4096 wavefronts, of 32 tokens at least.
+// How a problem is cut: one chunk of tokens per sequence unless the device would be half empty, then chunks for `held` wavefronts,
+// of 32 tokens at least and whole tiles; two channels to a lane (fewer instructions for each) where that still leaves `full` wavefronts.
 // From kJoin chunks on, a kernel of its own runs through them; up to there each wavefront does, all loads in flight.
-constexpr int kMostChunks = 128, kJoin = 9;
+constexpr int kMostChunks = 256, kJoin = 9;
 struct ScanPlan {
     int channels, states;
     int64_t column_blocks, chunk_tokens, chunks;
 };
-inline ScanPlan scan_plan(int64_t B, int64_t L, int64_t K, int64_t N, int64_t full) {
-    ScanPlan p{N <= 16 && B * ceil_div(K, 32) >= full ? 2 : 1, states_per_lane(N), 0, 0, 0};
+inline ScanPlan scan_plan(int64_t B, int64_t L, int64_t K, int64_t N, int64_t full, int64_t held, int tile) {
+    const int64_t most = ceil_div(L, 32) < kMostChunks ? ceil_div(L, 32) : kMostChunks;
+    const auto cut = [&](int64_t waves) { return waves >= 1024 ? (int64_t)1 : ceil_div(held, waves > 0 ? waves : 1) < most ? ceil_div(held, waves > 0 ? waves : 1) : most; };
+    const int64_t pairs = B * ceil_div(K, 32);
+    ScanPlan p{N <= 16 && pairs * cut(pairs) >= full ? 2 : 1, states_per_lane(N), 0, 0, 0};
     p.column_blocks = ceil_div(K, 16 * p.channels);
-    const int64_t waves = B * p.column_blocks;
-    int64_t chunks = waves >= 1024 ? 1 : ceil_div(4096, waves > 0 ? waves : 1);
-    if (chunks > ceil_div(L, 32)) chunks = ceil_div(L, 32);
-    if (chunks > kMostChunks) chunks = kMostChunks;
-    p.chunk_tokens = ceil_div(ceil_div(L, chunks), 16) * 16;
+    p.chunk_tokens = ceil_div(ceil_div(L, cut(B * p.column_blocks)), tile) * tile;
     p.chunks = ceil_div(L, p.chunk_tokens);
     return p;
 }
@@ -147,9 +146,10 @@ namespace {
 
 // Runs through the chunks of a sequence for every state.  A chunk's slot i holds what it leaves by itself, end(i), and its sum of D;
 // in(i + 1) = exp(a sum D(i)) in(i) + end(i) replaces end(i) (the first chunk's in is the state, or 0).  BACKWARD: the same from
-// the last chunk to the first.  16 lanes take adjacent states, 16 of those groups a run of chunks each: a run's values are
+// the last chunk to the first.  16 lanes take adjacent states, 32 of those groups a run of chunks each: a run's values are
 // loaded at once, the runs are joined through LDS, and then the run writes what comes into its chunks.
-constexpr int kJoinStates = 16, kJoinRuns = 16, kJoinRun = kMostChunks / kJoinRuns;
+constexpr int kJoinStates = 16, kJoinRuns = 32, kJoinRun = kMostChunks / kJoinRuns;
+__host__ __device__ inline int join_length(int steps) { return steps <= 4 * kJoinRuns ? 4 : kJoinRun; }  // (few runs: they are joined one after the other)
 template <bool BACKWARD>
 __global__ __launch_bounds__(kJoinStates *kJoinRuns) void join_chunks(float *__restrict__ chunk_state, const float *__restrict__ chunk_dt, const float *__restrict__ a,
                                                                      const float *__restrict__ state, int64_t channels, int K, int N, int chunks) {
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(kJoinStates *kJoinRuns) void join_chunks(float *__r
     const bool there = at < channels * N;
     const int64_t channel = there ? at / N : 0;
     const int steps = chunks - 1;                                    // chunks that leave something to another one
-    const int length = (steps + kJoinRuns - 1) / kJoinRuns, first = run * length;
+    const int length = join_length(steps), first = run * length;
     const float a2 = there ? a[channel % K * N + (at - channel * N)] * kLog2e : 0.0f;
     float end[kJoinRun], D[kJoinRun], h = 0.0f, sum = 0.0f;
 #pragma unroll
@@ -187,7 +187,8 @@ __global__ __launch_bounds__(kJoinStates *kJoinRuns) void join_chunks(float *__r
 template <bool BACKWARD, typename T>
 int launch_join_chunks(const ScanArgs<T> &s, hipStream_t stream) {
     const int64_t channels = (int64_t)s.B * s.K;
-    join_chunks<BACKWARD><<<dim3((unsigned)ceil_div(channels * s.N, kJoinStates)), dim3(kJoinStates * kJoinRuns), 0, stream>>>(
+    const int steps = (int)s.chunks - 1, runs = (int)ceil_div(ceil_div(steps, join_length(steps)), 4) * 4;  // (whole wavefronts)
+    join_chunks<BACKWARD><<<dim3((unsigned)ceil_div(channels * s.N, kJoinStates)), dim3(kJoinStates * runs), 0, stream>>>(
         s.chunk_state, s.chunk_dt, s.a, s.state, channels, s.K, s.N, (int)s.chunks);
     return check_launch("join_chunks");
 }

@@ -15,6 +15,7 @@ using namespace ptq4vm;
 
 constexpr int kTile = kMark;  // tokens that are staged together, and whose states are in registers
 constexpr int64_t kFull = 2048;  // wavefronts from which two channels to a lane are faster: 2 to a SIMD (3072: 275 us against 295)
+constexpr int64_t kHeld = 6144;  // wavefronts that sequences are cut for: three rounds of them (20000 x 1536, 2048: 786 us, 3072: 587, 6144: 543)
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // CARRY_ONLY: from a zero gradient behind the chunk, without outputs; leaves e^{D a} g at the chunk's first token and the sum
@@ -274,23 +275,23 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
 template <typename T>
 __global__ __launch_bounds__(256) void sum_column_blocks(const float *__restrict__ partial, int column_blocks, int64_t L, int64_t values, int N, Tokens<T> db,
                                                          Tokens<T> dc) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= values) return;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    int s = 0;
-    for (; s + 4 <= column_blocks; s += 4)
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < values; i += (int64_t)gridDim.x * 256) {
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        int s = 0;
+        for (; s + 4 <= column_blocks; s += 4)
 #pragma unroll
-        for (int j = 0; j < 4; j++) sum[j] += partial[(s + j) * values + i];
-    for (; s < column_blocks; s++) sum[0] += partial[s * values + i];
-    const float v = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    const int64_t row = i / (2 * N);
-    const int at = (int)(i - row * 2 * N);
-    const int b = (int)(row / L);
-    const int64_t t = row - b * L;
-    if (at < N)
-        db.at(b, t)[at] = (T)v;
-    else
-        dc.at(b, t)[at - N] = (T)v;
+            for (int j = 0; j < 4; j++) sum[j] += partial[(s + j) * values + i];
+        for (; s < column_blocks; s++) sum[0] += partial[s * values + i];
+        const float v = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        const int64_t row = i / (2 * N);
+        const int at = (int)(i - row * 2 * N);
+        const int b = (int)(row / L);
+        const int64_t t = row - b * L;
+        if (at < N)
+            db.at(b, t)[at] = (T)v;
+        else
+            dc.at(b, t)[at - N] = (T)v;
+    }
 }
 
 struct BackwardSizes {
@@ -306,7 +307,7 @@ extern "C" {
 
 int64_t ptq4vm_gated_scan_backward_workspace(int64_t B, int64_t L, int64_t K, int64_t N) {
     if (!scan_sizes(B, L, K, N) || B == 0) return 0;
-    const BackwardSizes s = backward_sizes(scan_plan(B, L, K, N, kFull), B, L, K, N);
+    const BackwardSizes s = backward_sizes(scan_plan(B, L, K, N, kFull, kHeld, kTile), B, L, K, N);
     return (s.bc + s.a + s.chunk) * 4;
 }
 
@@ -335,11 +336,10 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     const SumOut parameters{da, dd, ddt_bias, K * N, K};
     if (B == 0) return launch_sum_partials(nullptr, 0, K * (N + 2), parameters, stream);
-    const ScanPlan plan = scan_plan(B, L, K, N, kFull);
+    const ScanPlan plan = scan_plan(B, L, K, N, kFull, kHeld, kTile);
     const BackwardSizes sizes = backward_sizes(plan, B, L, K, N);
     float *const ws = static_cast<float *>(workspace);
     const int64_t values = B * L * 2 * N;
-    if (ceil_div(values, 256) > kMaxTokenRows) return PTQ4VM_ERR_SHAPE;
     const int rc = for_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
         ScanArgs<T> s{};
@@ -364,7 +364,7 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
             return go(std::false_type{}, plan.chunks);
         });
         if (e2) return e2;
-        sum_column_blocks<T><<<dim3((unsigned)ceil_div(values, 256)), dim3(256), 0, stream>>>(
+        sum_column_blocks<T><<<dim3((unsigned)(values < (int64_t)1 << 30 ? ceil_div(values, 256) : 1 << 22)), dim3(256), 0, stream>>>(
             ws, (int)plan.column_blocks, L, values, (int)N, tokens<T>(db, L, lddb, reverse), tokens<T>(dc, L, lddc, reverse));
         return check_launch("sum_column_blocks");
     });

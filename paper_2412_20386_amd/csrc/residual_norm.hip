@@ -281,17 +281,17 @@ __global__ __launch_bounds__(kSumThreads) void sum_norm_partials(const float *__
                                                                 uint32_t gate_blocks, const float *__restrict__ partial, int64_t rows, int64_t stride, int64_t cols,
                                                                 SumOut out) {
     if (blockIdx.x >= gate_blocks) return sum_columns(partial, rows, stride, cols, out, blockIdx.x - gate_blocks);
-    const int64_t i = (int64_t)blockIdx.x * kSumThreads + threadIdx.x;
-    if (i >= gates) return;
-    const int64_t g = i / K;
-    const float *from = gate_partial + g * parts * K + (i - g * K);
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    uint32_t s = 0;
-    for (; s + 4 <= parts; s += 4)
+    for (int64_t i = (int64_t)blockIdx.x * kSumThreads + threadIdx.x; i < gates; i += (int64_t)gate_blocks * kSumThreads) {
+        const int64_t g = i / K;
+        const float *from = gate_partial + g * parts * K + (i - g * K);
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        uint32_t s = 0;
+        for (; s + 4 <= parts; s += 4)
 #pragma unroll
-        for (int j = 0; j < 4; j++) sum[j] += from[(int64_t)(s + j) * K];
-    for (; s < parts; s++) sum[0] += from[(int64_t)s * K];
-    dgate[i] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            for (int j = 0; j < 4; j++) sum[j] += from[(int64_t)(s + j) * K];
+        for (; s < parts; s++) sum[0] += from[(int64_t)s * K];
+        dgate[i] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
 }
 
 // How a row is held: chunks loads of vec elements by 2^n lanes, or by 4, 8 or 16 wavefronts
@@ -448,8 +448,7 @@ int ptq4vm_residual_norm_backward(int dtype, int stream_dtype, const void *dy, c
         if (rc != PTQ4VM_OK) return rc;
     }
     const bool parts = gate && (M == 0 || gate_in_parts(c, gates));
-    const int64_t gate_blocks = parts ? ceil_div(G * K, kSumThreads) : 0, cols = w_post ? 2 * K : K;
-    if (gate_blocks > kMaxTokenRows / 2) return PTQ4VM_ERR_SHAPE;
+    const int64_t gate_blocks = !parts ? 0 : G * K < (int64_t)1 << 30 ? ceil_div(G * K, kSumThreads) : 1 << 20, cols = w_post ? 2 * K : K;
     sum_norm_partials<<<dim3((unsigned)(gate_blocks + ceil_div(cols, kSumCols))), dim3(kSumThreads), 0, stream>>>(
         gate_partial, dgate, G * K, (int)K, c.parts, (uint32_t)gate_blocks, partial, c.blocks, 2 * K, cols, {dw, dw_post, nullptr, K, K});
     return check_launch("sum_norm_partials");

@@ -283,7 +283,7 @@ int conv(int dtype, const void *x, const float *w, const float *bias, const void
         while (a.run > 4 && per_token * ceil_div(L, a.run) < 8 * 256 * 64) a.run /= 2;
         a.runs = ceil_div(L, a.run);
         const int64_t blocks = ceil_div(a.runs * B, kThreads >> a.lanes_log2) * a.column_blocks;
-        if (blocks > kMaxTokenRows) return (int)PTQ4VM_ERR_SHAPE;
+        if (!grid_fits(blocks, kThreads)) return (int)PTQ4VM_ERR_SHAPE;
         return for_filter(W, K % kVec == 0, [&](auto taps, auto whole) {
             token_conv_runs<T, taps(), whole()><<<dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream)>>>(a);
             return check_launch("token_conv_runs");

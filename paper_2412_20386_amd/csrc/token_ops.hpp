@@ -9,6 +9,8 @@
 namespace ptq4vm {
 
 constexpr int64_t kMaxTokenRows = 0x7fffffff;  // rows and widths are 32-bit in the kernels, offsets 64-bit
+// Whether a grid of one dimension can be launched: it holds fewer than 2^32 threads
+inline bool grid_fits(int64_t blocks, int threads) { return blocks * threads < ((int64_t)1 << 32); }
 
 inline bool valid_dtype(int dtype) { return dtype == PTQ4VM_F16 || dtype == PTQ4VM_BF16 || dtype == PTQ4VM_F32; }
 inline uintptr_t dtype_bytes(int dtype) { return dtype == PTQ4VM_F32 ? 4 : 2; }

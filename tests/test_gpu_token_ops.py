@@ -82,6 +82,10 @@ SCANS = [
     (1, 197, 48, 16, "f16", False, True, 12, True, True, True),
     (1, 600, 18, 16, "f32", True, True, 0, True, True, True),
     (2, 1057, 5, 2, "f16", False, True, 0, True, True, True),
+    (1, 9001, 3, 2, "f32", False, True, 0, True, True, True),     # as many chunks as there can be
+    (1, 3000, 70, 16, "bf16", True, False, 0, True, True, True),
+    (2, 256, 30, 11, "f16", False, True, 2, True, True, True),    # every tile of a sequence in one workgroup
+    (5, 257, 20, 16, "f32", True, True, 0, True, True, True),
     (64, 3, 1030, 16, "f16", False, True, 0, True, True, True),   # two channels to a lane
     (70, 18, 992, 13, "bf16", True, False, 0, True, True, True),
 ]

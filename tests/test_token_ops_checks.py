@@ -86,6 +86,8 @@ def test_sizes(lib, name):
         assert call(lib, name, G=3) == SHAPE and call(lib, name, G=0) == SHAPE and call(lib, name, G=-2) == SHAPE
         assert call(lib, name, K=16385) == SHAPE
         assert call(lib, name, dtype=0, stream_dtype=1) == SHAPE and call(lib, name, dtype=2, stream_dtype=0) == SHAPE
+    if name == "gated_scan_step":
+        assert call(lib, name, B=1 << 24, K=1, ldu=1, lddt=1, ldz=1, ldy=1) == SHAPE  # more threads than a grid holds
     # B * L beyond 31 bits, each of them below
     if "L" in sizes:
         assert call(lib, name, B=1 << 20, L=1 << 20) == SHAPE
