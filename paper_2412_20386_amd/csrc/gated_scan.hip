@@ -7,6 +7,7 @@ using namespace ptq4vm;
 
 constexpr int kTile = 16;           // tokens that are staged together
 constexpr int64_t kFull = 4096;     // wavefronts from which two channels to a lane are faster: 4 to a SIMD (3072: 112 us against 102)
+constexpr int64_t kFullWide = 4096; // wavefronts from which a channel to a lane is faster: 4 to a SIMD (1536: 128 us against 102)
 constexpr int64_t kHeld = 6144;     // wavefronts that sequences are cut for (16384 x 768: 2048 134 us, 4096 110, 5120 103, 6144 102)
 
 // One wavefront: 16 C channels of one sequence through the tokens of one chunk.
@@ -144,6 +145,113 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
         }
 }
 
+// The same with a channel's 16 states in one lane, 64 channels to a wavefront: no sums over lanes, and the products D u b of a
+// token, an outer product of 4 channels and 4 states for every quad of lanes, come with the addition to e^{D a} h from the matrix
+// pipe (v_mfma_f32_4x4x1: 16 products for an instruction of a lane's 4, and the vector ALU is what bounds this kernel).  An exponential and three
+// instructions a state and a quarter, against an exponential, four and the sums' seven eighths: 256 x 197 x 1536 takes 274 us, with
+// two channels to a lane 287.  (118 registers, four wavefronts to a SIMD; squeezed into five or six it spills: 377 and 415 us.)
+constexpr int kWideTile = 8;  // tokens that are staged together
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <typename T, bool RAGGED>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(4))) void gated_scan_wide(ScanArgs<T> p) {
+    using S = ScanLane<4, 4, kWideTile>;
+    constexpr int V = S::kVec;
+    static_assert(S::kChannels == 64 && S::kStates == 16, "a lane to a channel");
+    alignas(16) __shared__ float steps[kWideTile][64];  // D; then s without its d u
+    alignas(16) __shared__ float inputs[kWideTile][64];  // D u
+    alignas(16) __shared__ float sb[kWideTile][4][4];    // state n at [n % 4][n / 4]: what lane n % 4 of a quad gives to the products
+    alignas(16) __shared__ float sc[kWideTile][16];
+    alignas(16) __shared__ float bias[64], skip[64];
+    const uint32_t block = xcd_contiguous(blockIdx.x, p.blocks);
+    if (block >= p.blocks) return;
+    const int cb = block % p.column_blocks, b = block / p.column_blocks, lane = threadIdx.x, kc = cb * 64 + lane;
+    const bool mine = !RAGGED || kc < p.K;
+
+    f32x4 a2[4], h[4];
+    const auto load_states_of = [&](const float *from, int64_t channel, f32x4 (&to)[4]) {
+        float v[16];
+        load_channel<16, true>(from, channel, 0, RAGGED ? p.N : 16, mine, v);
+#pragma unroll
+        for (int i = 0; i < 16; i++) to[i / 4][i % 4] = v[i];
+    };
+    const auto store_states_of = [&](float *to, int64_t channel) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; i++) v[i] = h[i / 4][i % 4];
+        store_channel<16, true>(to, channel, 0, RAGGED ? p.N : 16, mine, v);
+    };
+    load_states_of(p.a, kc, a2);
+#pragma unroll
+    for (int m = 0; m < 4; m++) a2[m] *= kLog2e, h[m] = 0.0f;
+    if (p.state) load_states_of(p.state, (int64_t)b * p.K + kc, h);
+    const int vt = lane / S::kAcross, vk = (lane % S::kAcross) * V, k = cb * 64 + vk, nk = max(0, min(V, p.K - k));
+    bias[lane] = p.dt_bias && kc < p.K ? p.dt_bias[kc] : 0.0f;
+    skip[lane] = p.d && kc < p.K ? p.d[kc] : 0.0f;
+    __syncthreads();
+    T ru[V], rdt[V], rz[V], rb[S::kStateVec], rc[S::kStateVec];
+    const auto fetch = [&](int64_t t0) {
+        const int last = (int)min((int64_t)kWideTile, p.L - t0) - 1;
+        load_token<V, RAGGED>(p.u, b, t0, vt, last, k, nk, ru);
+        load_token<V, RAGGED>(p.dt, b, t0, vt, last, k, nk, rdt);
+        if (p.z.data) load_token<V, RAGGED>(p.z, b, t0, vt, last, k, nk, rz);
+        load_states<S, RAGGED>(p.b, b, t0, last, p.N, rb);
+        load_states<S, RAGGED>(p.c, b, t0, last, p.N, rc);
+    };
+    fetch(0);
+    for (int64_t t0 = 0; t0 < p.L; t0 += kWideTile) {
+        T u[V], z[V];
+        const bool there = t0 + vt < p.L;  // (tokens behind the last change nothing: D = 0)
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            u[i] = ru[i];
+            z[i] = rz[i];
+            const float D = softplus_of((float)rdt[i] + bias[vk + i]);
+            steps[vt][vk + i] = D, inputs[vt][vk + i] = D * (float)ru[i];
+        }
+        if (!there)
+#pragma unroll
+            for (int i = 0; i < V; i++) steps[vt][vk + i] = inputs[vt][vk + i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::kStateVec; i++) {
+            const int n = lane % 8 * S::kStateVec + i;
+            sb[lane / 8][n % 4][n / 4] = (float)rb[i];
+            sc[lane / 8][n] = (float)rc[i];
+        }
+        __syncthreads();
+        if (t0 + kWideTile < p.L) fetch(t0 + kWideTile);  // in flight under this tile's steps
+        static_assert(kWideTile == kMark, "a mark before every tile");
+        if (p.marks) store_states_of(p.marks, ((t0 / kMark) * p.B + b) * p.K + kc);
+#pragma unroll
+        for (int t = 0; t < kWideTile; t++) {
+            const float D = steps[t][lane], Du = inputs[t][lane];
+            f32x4 v = 0.0f;
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                f32x4 e;
+#pragma unroll
+                for (int i = 0; i < 4; i++) e[i] = __builtin_amdgcn_exp2f(a2[m][i] * D) * h[m][i];
+                h[m] = __builtin_amdgcn_mfma_f32_4x4x1f32(sb[t][lane & 3][m], Du, e, 0, 0, 0);
+                if (RAGGED)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) h[m][i] = m * 4 + i < p.N ? h[m][i] : 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] = fmaf(h[m][i], sc[t][m * 4 + i], v[i]);
+            }
+            steps[t][lane] = (v[0] + v[1]) + (v[2] + v[3]);
+        }
+        __syncthreads();
+        float y[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) y[i] = fmaf(skip[vk + i], (float)u[i], steps[vt][vk + i]);
+        if (p.z.data)
+#pragma unroll
+            for (int i = 0; i < V; i++) y[i] *= (float)z[i] * sigmoid_of((float)z[i]);
+        if (there) store_token<V, RAGGED>(p.y, b, t0, vt, k, nk, y);
+        __syncthreads();
+    }
+    if (p.state_out) store_states_of(p.state_out, (int64_t)b * p.K + kc);
+}
+
 // Few short sequences of few channels, up to 16 states: a lane takes one state, a wavefront 4 channels of one tile of tokens, a
 // workgroup all tiles of a sequence.  The tiles run side by side from a zero state, tell each other through LDS what they leave and
 // their sums of D, and run again from their true first states on what is staged already: one launch, and of the tokens'
@@ -246,6 +354,14 @@ __global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
     if (q == 0) p.y.at(b, 0)[k] = (T)v;
 }
 
+ScanPlan forward_plan(int64_t B, int64_t L, int64_t K, int64_t N) {
+    if (N > 4 && N <= 16 && B * ceil_div(K, 64) >= kFullWide) {
+        const int64_t column_blocks = ceil_div(K, 64);
+        return {4, 4, column_blocks, ceil_div(L, kWideTile) * kWideTile, 1};
+    }
+    return scan_plan(B, L, K, N, kFull, kHeld, kTile);
+}
+
 // Whether the tiles of a sequence run side by side in one workgroup: up to three workgroups on a compute unit (197 tokens x 1536
 // channels, us against chunks or one wavefront a sequence: 1 image 8.1 / 12.0, 2 images 11.9 / 15.2, 3 images 18.5 / 16.7)
 bool is_short(int64_t B, int64_t L, int64_t K, int64_t N) {
@@ -283,7 +399,7 @@ extern "C" {
 
 int64_t ptq4vm_gated_scan_workspace(int64_t B, int64_t L, int64_t K, int64_t N) {
     if (!scan_sizes(B, L, K, N) || B == 0) return 0;
-    const ScanPlan plan = scan_plan(B, L, K, N, kFull, kHeld, kTile);
+    const ScanPlan plan = forward_plan(B, L, K, N);
     return plan.chunks > 1 && !is_short(B, L, K, N) ? plan.chunks * B * K * (N + 1) * 4 : 0;
 }
 
@@ -297,7 +413,7 @@ int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, 
     if (workspace_bytes < need) return PTQ4VM_ERR_SHAPE;
     if (!aligned_to(state, 4) || !aligned_to(state_out, 4) || !aligned_to(marks, 4) || !aligned_to(workspace, 16)) return PTQ4VM_ERR_ALIGN;
     if (B == 0) return PTQ4VM_OK;
-    const ScanPlan plan = scan_plan(B, L, K, N, kFull, kHeld, kTile);
+    const ScanPlan plan = forward_plan(B, L, K, N);
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     return for_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
@@ -313,6 +429,14 @@ int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, 
             else
                 gated_scan_short<T, true><<<grid, block, 0, stream>>>(s);
             return check_launch("gated_scan_short");
+        }
+        if (plan.channels == 4) {
+            s.blocks = (uint32_t)(B * plan.column_blocks);
+            if (N == 16 && K % 64 == 0)
+                gated_scan_wide<T, false><<<dim3(xcd_grid(s.blocks)), dim3(64), 0, stream>>>(s);
+            else
+                gated_scan_wide<T, true><<<dim3(xcd_grid(s.blocks)), dim3(64), 0, stream>>>(s);
+            return check_launch("gated_scan_wide");
         }
         return for_layout(plan, K, N, [&](auto ns, auto ch, auto ragged) {
             const auto go = [&](auto states_only, int64_t chunks) {

@@ -86,6 +86,9 @@ SCANS = [
     (1, 3000, 70, 16, "bf16", True, False, 0, True, True, True),
     (2, 256, 30, 11, "f16", False, True, 2, True, True, True),    # every tile of a sequence in one workgroup
     (5, 257, 20, 16, "f32", True, True, 0, True, True, True),
+    (4100, 3, 64, 16, "f16", True, True, 0, True, True, True),    # a channel to a lane
+    (4100, 10, 7, 13, "bf16", False, True, 3, True, True, True),
+    (2050, 17, 66, 6, "f32", False, False, 0, False, True, True),
     (64, 3, 1030, 16, "f16", False, True, 0, True, True, True),   # two channels to a lane
     (70, 18, 992, 13, "bf16", True, False, 0, True, True, True),
 ]

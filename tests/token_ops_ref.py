@@ -39,7 +39,9 @@ def scan_backward(dy, u, dt, a, b, c, d, z, dt_bias, state=None, magnitude=False
     G, dz = f(dy), None
     if z is not None:
         G = f(dy) * f(z * sigmoid(z))
-        dz = f(dy) * s * f(sigmoid(z) * (1 + z * (1 - sigmoid(z))))
+        # the gate's derivative is a sum of sigma(z) and z sigma(z) (1 - sigma(z)), which cancel near z = -1.28: each term is rounded in
+        # proportion to itself, so the error there is that of the terms, not of their difference
+        dz = f(dy) * s * (sigmoid(z) + f(z * sigmoid(z) * (1 - sigmoid(z))))
     e = torch.exp(D[..., None] * a)
     g, carry = torch.zeros_like(h[:, 1:]), torch.zeros_like(h[:, 0])
     for t in reversed(range(L)):
