@@ -146,10 +146,10 @@ namespace {
 
 // Runs through the chunks of a sequence for every state.  A chunk's slot i holds what it leaves by itself, end(i), and its sum of D;
 // in(i + 1) = exp(a sum D(i)) in(i) + end(i) replaces end(i) (the first chunk's in is the state, or 0).  BACKWARD: the same from
-// the last chunk to the first.  16 lanes take adjacent states, 32 of those groups a run of chunks each: a run's values are
+// the last chunk to the first.  32 lanes take adjacent states, up to 16 of those groups a run of chunks each: a run's values are
 // loaded at once, the runs are joined through LDS, and then the run writes what comes into its chunks.
-constexpr int kJoinStates = 16, kJoinRuns = 32, kJoinRun = kMostChunks / kJoinRuns;
-__host__ __device__ inline int join_length(int steps) { return steps <= 4 * kJoinRuns ? 4 : kJoinRun; }  // (few runs: they are joined one after the other)
+constexpr int kJoinStates = 32, kJoinRuns = 16, kJoinRun = kMostChunks / kJoinRuns;
+__host__ __device__ inline int join_length(int steps) { return steps <= 4 * kJoinRuns ? 4 : steps <= 8 * kJoinRuns ? 8 : kJoinRun; }  // (few runs: they are joined one after the other)
 template <bool BACKWARD>
 __global__ __launch_bounds__(kJoinStates *kJoinRuns) void join_chunks(float *__restrict__ chunk_state, const float *__restrict__ chunk_dt, const float *__restrict__ a,
                                                                      const float *__restrict__ state, int64_t channels, int K, int N, int chunks) {
