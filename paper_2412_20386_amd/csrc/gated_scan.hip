@@ -355,7 +355,7 @@ __global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
 }
 
 ScanPlan forward_plan(int64_t B, int64_t L, int64_t K, int64_t N) {
-    if (N > 4 && N <= 16 && B * ceil_div(K, 64) >= kFullWide) {
+    if (N > 8 && N <= 16 && B * ceil_div(K, 64) >= kFullWide) {
         const int64_t column_blocks = ceil_div(K, 64);
         return {4, 4, column_blocks, ceil_div(L, kWideTile) * kWideTile, 1};
     }
@@ -477,7 +477,9 @@ int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float
         const auto with = [&](auto ns) { return N == 4 * ns() ? go(ns, std::false_type{}) : go(ns, std::true_type{}); };
         switch (states_per_lane(N)) {
             case 1: return with(integral_constant<int, 1>{});
+            case 2: return with(integral_constant<int, 2>{});
             case 4: return with(integral_constant<int, 4>{});
+            case 8: return with(integral_constant<int, 8>{});
             default: return with(integral_constant<int, 16>{});
         }
     });

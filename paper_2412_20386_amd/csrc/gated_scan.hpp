@@ -43,8 +43,8 @@ struct ScanLane {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// States of a quad's lane: 1, 4 or 16
-inline int states_per_lane(int64_t N) { return N <= 4 ? 1 : N <= 16 ? 4 : 16; }
+// States of a quad's lane: the power of two that has room for N
+inline int states_per_lane(int64_t N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 
 // How a problem is cut: one chunk of tokens per sequence unless the device would be half empty, then chunks for `held` wavefronts,
 // of 32 tokens at least and whole tiles; two channels to a lane (fewer instructions for each) where that still leaves `full` wavefronts.
@@ -71,9 +71,17 @@ int for_layout(const ScanPlan &p, int64_t K, int64_t N, F &&f) {
     using std::bool_constant;
     using std::integral_constant;
     const auto with = [&](auto ns, auto c) { return N == 4 * ns() && K % (16 * c()) == 0 ? f(ns, c, bool_constant<false>{}) : f(ns, c, bool_constant<true>{}); };
-    if (p.states == 16) return with(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    if (p.channels == 2) return p.states == 4 ? with(integral_constant<int, 4>{}, integral_constant<int, 2>{}) : with(integral_constant<int, 1>{}, integral_constant<int, 2>{});
-    return p.states == 4 ? with(integral_constant<int, 4>{}, integral_constant<int, 1>{}) : with(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+    constexpr integral_constant<int, 1> one{};
+    constexpr integral_constant<int, 2> two{};
+    constexpr integral_constant<int, 4> four{};
+    const auto pairs = [&](auto ns) { return p.channels == 2 ? with(ns, two) : with(ns, one); };
+    switch (p.states) {
+        case 1: return pairs(one);
+        case 2: return pairs(two);
+        case 4: return pairs(four);
+        case 8: return with(integral_constant<int, 8>{}, one);
+        default: return with(integral_constant<int, 16>{}, one);
+    }
 }
 
 // Sizes that every entry point takes

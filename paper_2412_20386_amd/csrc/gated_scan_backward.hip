@@ -21,7 +21,7 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // CARRY_ONLY: from a zero gradient behind the chunk, without outputs; leaves e^{D a} g at the chunk's first token and the sum
 // of D, from which the chunks before it know the gradient that comes in.
 template <typename T, int NS, int C, bool RAGGED, bool CARRY_ONLY>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 1 : CARRY_ONLY ? 4 : C == 1 ? 3 : 2))) void gated_scan_backward_tokens(ScanArgs<T> p) {
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 1 : CARRY_ONLY ? 4 : NS * C > 4 ? 2 : 3))) void gated_scan_backward_tokens(ScanArgs<T> p) {
     using S = ScanLane<NS, C, kTile>;
     constexpr int V = S::kVec;
     alignas(16) __shared__ float2 steps[kTile][S::kChannels];  // D and D u, then sum g b

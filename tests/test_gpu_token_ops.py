@@ -88,7 +88,11 @@ SCANS = [
     (5, 257, 20, 16, "f32", True, True, 0, True, True, True),
     (4100, 3, 64, 16, "f16", True, True, 0, True, True, True),    # a channel to a lane
     (4100, 10, 7, 13, "bf16", False, True, 3, True, True, True),
-    (2050, 17, 66, 6, "f32", False, False, 0, False, True, True),
+    (2, 70, 21, 32, "f16", False, True, 0, True, True, True),
+    (3, 70, 16, 24, "bf16", True, False, 1, True, False, True),
+    (40, 18, 1700, 7, "f16", False, True, 0, True, True, True),
+    (1, 300, 33, 8, "f32", True, True, 0, True, True, True),
+    (2050, 17, 66, 10, "f32", False, False, 0, False, True, True),
     (64, 3, 1030, 16, "f16", False, True, 0, True, True, True),   # two channels to a lane
     (70, 18, 992, 13, "bf16", True, False, 0, True, True, True),
 ]
@@ -135,7 +139,7 @@ def test_scan(case):
         _near(_time(got.cpu(), B, L, reverse) if by_token else got, want[name], size[name], 2 * r + (K if name in ("db", "dc") else B * L), (dtype, "T" if by_token else "f32", name))
 
 
-@pytest.mark.parametrize("B,K,N,dtype,gate", [(1, 1, 1, "f32", True), (3, 50, 16, "f16", True), (2, 33, 5, "bf16", False), (5, 20, 64, "f16", True), (2, 70, 3, "f32", True), (2, 9, 37, "bf16", True)])
+@pytest.mark.parametrize("B,K,N,dtype,gate", [(1, 1, 1, "f32", True), (3, 50, 16, "f16", True), (2, 33, 5, "bf16", False), (5, 20, 64, "f16", True), (5, 20, 30, "bf16", True), (3, 30, 8, "f16", True), (2, 70, 3, "f32", True), (2, 9, 37, "bf16", True)])
 def test_scan_step_by_step_is_the_scan(B, K, N, dtype, gate):
     """Token by token, in place, against the definition; and the step's own results against those of the scan over one token."""
     L, T = 9, TYPES[dtype]
