@@ -359,7 +359,8 @@ ScanPlan forward_plan(int64_t B, int64_t L, int64_t K, int64_t N) {
         const int64_t column_blocks = ceil_div(K, 64);
         return {4, 4, column_blocks, ceil_div(L, kWideTile) * kWideTile, 1};
     }
-    return scan_plan(B, L, K, N, kFull, kHeld, kTile);
+    // (32 x 197 x 768 whole and one channel to a lane 38 us, in chunks and two 52; 16 x 4000 x 1536 708 and 629)
+    return scan_plan(B, L, K, N, kFull, kHeld, kTile, L < 1024);
 }
 
 // Whether the tiles of a sequence run side by side in one workgroup: up to three workgroups on a compute unit (197 tokens x 1536

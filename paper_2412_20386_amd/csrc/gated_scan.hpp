@@ -47,18 +47,19 @@ constexpr float kLog2e = 1.44269504088896340736f;
 inline int states_per_lane(int64_t N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 
 // How a problem is cut: one chunk of tokens per sequence unless the device would be half empty, then chunks for `held` wavefronts,
-// of 32 tokens at least and whole tiles; two channels to a lane (fewer instructions for each) where that still leaves `full` wavefronts.
+// of 32 tokens at least and whole tiles; two channels to a lane (fewer instructions for each) where that still leaves `full` wavefronts;
+// not at the price of chunks if `whole`.
 // From kJoin chunks on, a kernel of its own runs through them; up to there each wavefront does, all loads in flight.
 constexpr int kMostChunks = 256, kJoin = 9;
 struct ScanPlan {
     int channels, states;
     int64_t column_blocks, chunk_tokens, chunks;
 };
-inline ScanPlan scan_plan(int64_t B, int64_t L, int64_t K, int64_t N, int64_t full, int64_t held, int tile) {
+inline ScanPlan scan_plan(int64_t B, int64_t L, int64_t K, int64_t N, int64_t full, int64_t held, int tile, bool whole) {
     const int64_t most = ceil_div(L, 32) < kMostChunks ? ceil_div(L, 32) : kMostChunks;
     const auto cut = [&](int64_t waves) { return waves >= 1024 ? (int64_t)1 : ceil_div(held, waves > 0 ? waves : 1) < most ? ceil_div(held, waves > 0 ? waves : 1) : most; };
-    const int64_t pairs = B * ceil_div(K, 32);
-    ScanPlan p{N <= 16 && pairs * cut(pairs) >= full ? 2 : 1, states_per_lane(N), 0, 0, 0};
+    const int64_t pairs = B * ceil_div(K, 32), singles = B * ceil_div(K, 16);
+    ScanPlan p{N <= 16 && (whole && cut(singles) == 1 ? pairs : pairs * cut(pairs)) >= full ? 2 : 1, states_per_lane(N), 0, 0, 0};
     p.column_blocks = ceil_div(K, 16 * p.channels);
     p.chunk_tokens = ceil_div(ceil_div(L, cut(B * p.column_blocks)), tile) * tile;
     p.chunks = ceil_div(L, p.chunk_tokens);

@@ -294,6 +294,9 @@ __global__ __launch_bounds__(256) void sum_column_blocks(const float *__restrict
     }
 }
 
+// (24 x 197 x 768 in chunks and two channels to a lane 91 us, whole and one 114)
+ScanPlan backward_plan(int64_t B, int64_t L, int64_t K, int64_t N) { return scan_plan(B, L, K, N, kFull, kHeld, kTile, false); }
+
 struct BackwardSizes {
     int64_t bc, a, chunk;  // floats
 };
@@ -307,7 +310,7 @@ extern "C" {
 
 int64_t ptq4vm_gated_scan_backward_workspace(int64_t B, int64_t L, int64_t K, int64_t N) {
     if (!scan_sizes(B, L, K, N) || B == 0) return 0;
-    const BackwardSizes s = backward_sizes(scan_plan(B, L, K, N, kFull, kHeld, kTile), B, L, K, N);
+    const BackwardSizes s = backward_sizes(backward_plan(B, L, K, N), B, L, K, N);
     return (s.bc + s.a + s.chunk) * 4;
 }
 
@@ -336,7 +339,7 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     const SumOut parameters{da, dd, ddt_bias, K * N, K};
     if (B == 0) return launch_sum_partials(nullptr, 0, K * (N + 2), parameters, stream);
-    const ScanPlan plan = scan_plan(B, L, K, N, kFull, kHeld, kTile);
+    const ScanPlan plan = backward_plan(B, L, K, N);
     const BackwardSizes sizes = backward_sizes(plan, B, L, K, N);
     float *const ws = static_cast<float *>(workspace);
     const int64_t values = B * L * 2 * N;
