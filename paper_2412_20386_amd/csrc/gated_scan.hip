@@ -6,9 +6,9 @@ namespace {
 using namespace ptq4vm;
 
 constexpr int kTile = 16;           // tokens that are staged together
-constexpr int64_t kFull = 4096;     // wavefronts from which two channels to a lane are faster: 4 to a SIMD (3072: 112 us against 102)
-constexpr int64_t kFullWide = 4096; // wavefronts from which a channel to a lane is faster: 4 to a SIMD (1536: 128 us against 102)
-constexpr int64_t kHeld = 6144;     // wavefronts that sequences are cut for (16384 x 768: 2048 134 us, 4096 110, 5120 103, 6144 102)
+constexpr int64_t kFull = 4096;     // wavefronts from which two channels to a lane are faster: 4 to a SIMD (at 3 to a SIMD 112 us against 102)
+constexpr int64_t kFullWide = 4096; // wavefronts from which a channel to a lane is faster: 4 to a SIMD (at 1.5 to a SIMD 128 us against 102)
+constexpr int64_t kHeld = 6144;     // wavefronts that sequences are cut for (16384 x 768: 2048 134 us, 4096 110, 5120 103, 6144 99)
 
 // One wavefront: 16 C channels of one sequence through the tokens of one chunk.
 // STATES_ONLY: from a zero state, without outputs; leaves the chunk's end state and its sum of D, from which the chunks behind
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
 constexpr int kWideTile = 8;  // tokens that are staged together
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename T, bool RAGGED>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(4))) void gated_scan_wide(ScanArgs<T> p) {
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(RAGGED && sizeof(T) == 4 ? 3 : 4))) void gated_scan_wide(ScanArgs<T> p) {
     using S = ScanLane<4, 4, kWideTile>;
     constexpr int V = S::kVec;
     static_assert(S::kChannels == 64 && S::kStates == 16, "a lane to a channel");

@@ -14,14 +14,14 @@ namespace {
 using namespace ptq4vm;
 
 constexpr int kTile = kMark;  // tokens that are staged together, and whose states are in registers
-constexpr int64_t kFull = 2048;  // wavefronts from which two channels to a lane are faster: 2 to a SIMD (3072: 275 us against 295)
-constexpr int64_t kHeld = 6144;  // wavefronts that sequences are cut for: three rounds of them (20000 x 1536, 2048: 786 us, 3072: 587, 6144: 543)
+constexpr int64_t kFull = 2048;  // wavefronts from which two channels to a lane are faster: 2 to a SIMD (at 3 to a SIMD 275 us against 295)
+constexpr int64_t kHeld = 6144;  // wavefronts that sequences are cut for: three rounds of them (20000 x 1536, one round: 786 us, one and a half: 587, three: 543)
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // CARRY_ONLY: from a zero gradient behind the chunk, without outputs; leaves e^{D a} g at the chunk's first token and the sum
 // of D, from which the chunks before it know the gradient that comes in.
 template <typename T, int NS, int C, bool RAGGED, bool CARRY_ONLY>
-__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 1 : CARRY_ONLY ? 4 : NS * C > 4 ? 2 : 3))) void gated_scan_backward_tokens(ScanArgs<T> p) {
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 1 : CARRY_ONLY ? 4 : NS * C > 4 || (C == 2 && NS > 1) ? 2 : 3))) void gated_scan_backward_tokens(ScanArgs<T> p) {
     using S = ScanLane<NS, C, kTile>;
     constexpr int V = S::kVec;
     alignas(16) __shared__ float2 steps[kTile][S::kChannels];  // D and D u, then sum g b
