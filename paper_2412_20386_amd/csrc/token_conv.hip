@@ -5,7 +5,9 @@
 //
 // Bound by memory (2 - 12 flops a byte).  A lane owns 8 adjacent channels (16 bytes of 16-bit elements) and walks over a run of tokens with
 // the window of W - 1 earlier ones in registers, so that a token is read once by its run; the next run reads the last W - 1
-// again (from the L2: neighbouring runs are neighbours in a workgroup).  Sums are fp32.
+// again (from the L2: neighbouring runs are neighbours in a workgroup).  Sums are fp32.  Forward, 128 x 197 x 768 in fp16: 21 us,
+// 3.7 TB/s (one round of wavefronts, whose first loads nothing hides); backward, 64 x 197 x 1536 in bf16: 37 us, 3.2 TB/s, 4.8 of
+// them the sums of the filters' gradients.
 #include <type_traits>
 
 #include "token_ops.hpp"
