@@ -327,31 +327,45 @@ __global__ __launch_bounds__(kShortTiles * 64) void gated_scan_short(ScanArgs<T>
 }
 
 // One token of every sequence: bound by the states, which are read and written once (128 bytes of a channel's 16 against 10
-// of everything else).  A quad of lanes takes a channel, its lanes adjacent states; a workgroup 64 channels of one sequence.  A
-// lane's states are read before they are written by it alone, so state_out may be the state's own buffer.  1000 sequences x 1536 x 16:
-// 43.5 us, 4.8 TB/s.
-template <typename T, int NS, bool RAGGED>
+// of everything else).  LANES lanes take a channel, 4 adjacent states each (16 bytes), a quad the next 16 of it after that; a
+// workgroup 256 / LANES channels of one sequence.  A lane's states are read before they are written by it alone, so state_out may be
+// the state's own buffer.  1000 sequences x 1536 x 16: 44 us, 4.8 TB/s; 3868 x 1408 x 4: 44 us, 5.0 TB/s (88 us with a state to each
+// lane of a quad).
+template <typename T, int LANES, int GROUPS, bool RAGGED>
 __global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
-    const int b = blockIdx.x / p.column_blocks, k = (int)(blockIdx.x - b * p.column_blocks) * 64 + (threadIdx.x >> 2);
-    const int q = threadIdx.x & 3, n0 = q * NS, n = RAGGED ? max(0, min(NS, p.N - n0)) : NS;
-    if (k >= p.K) return;  // (whole quads)
-    float h[NS], a[NS];
-    T B[NS], CC[NS];
-    load_channel<NS, RAGGED>(p.state, (int64_t)b * p.K + k, n0, p.N, true, h);
-    load_channel<NS, RAGGED>(p.a, k, n0, p.N, true, a);
-    load_first<NS>(p.b.at(b, 0) + n0, n, B);
-    load_first<NS>(p.c.at(b, 0) + n0, n, CC);
+    const int b = blockIdx.x / p.column_blocks, k = (int)(blockIdx.x - b * p.column_blocks) * (256 / LANES) + threadIdx.x / LANES;
+    const int q = threadIdx.x % LANES;
+    if (k >= p.K) return;  // (all lanes of a channel)
+    float h[GROUPS][4], a[GROUPS][4];
+    T B[GROUPS][4], CC[GROUPS][4];
+    int n[GROUPS];
+    const int N = RAGGED ? p.N : 4 * LANES * GROUPS;
+    const int64_t channel = (int64_t)k * N + q * 4, at = (int64_t)b * p.K * N + channel;
+    const T *const from_b = p.b.at(b, 0) + q * 4, *const from_c = p.c.at(b, 0) + q * 4;
+#pragma unroll
+    for (int j = 0; j < GROUPS; j++) {
+        const int first = j * LANES * 4;
+        n[j] = RAGGED ? max(0, min(4, N - first - q * 4)) : 4;
+        load_first<4>(p.state + at + first, n[j], h[j]);
+        load_first<4>(p.a + channel + first, n[j], a[j]);
+        load_first<4>(from_b + first, n[j], B[j]);
+        load_first<4>(from_c + first, n[j], CC[j]);
+    }
     const float u = (float)p.u.at(b, 0)[k];
     const float D = softplus_of((float)p.dt.at(b, 0)[k] + (p.dt_bias ? p.dt_bias[k] : 0.0f)), Du = D * u;
     const float z = p.z.data ? (float)p.z.at(b, 0)[k] : 0.0f;
     float v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NS; i++) {
-        h[i] = fmaf(__builtin_amdgcn_exp2f(a[i] * kLog2e * D), h[i], Du * (float)B[i]);
-        v = i < n ? fmaf(h[i], (float)CC[i], v) : v;
+    for (int j = 0; j < GROUPS; j++) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            h[j][i] = fmaf(__builtin_amdgcn_exp2f(a[j][i] * kLog2e * D), h[j][i], Du * (float)B[j][i]);
+            v = i < n[j] ? fmaf(h[j][i], (float)CC[j][i], v) : v;
+        }
+        store_first<4>(p.state_out + at + j * LANES * 4, n[j], h[j]);
     }
-    store_channel<NS, RAGGED>(p.state_out, (int64_t)b * p.K + k, n0, p.N, true, h);
-    v = quad_sum(v);
+    if constexpr (LANES >= 2) v = add_dpp<0xB1>(v);
+    if constexpr (LANES == 4) v = add_dpp<0x4E>(v);
     if (p.d) v = fmaf(p.d[k], u, v);
     if (p.z.data) v *= z * sigmoid_of(z);
     if (q == 0) p.y.at(b, 0)[k] = (T)v;
@@ -472,20 +486,22 @@ int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float
         using T = decltype(zero);
         ScanArgs<T> s = scan_args<T>(u, dt, a, b, c, d, z, dt_bias, y, false, B, 1, K, N, ldu, lddt, ldb, ldc, ldz, ldy);
         s.state = state, s.state_out = state_out;
-        s.column_blocks = (int)ceil_div(K, 64);
         using std::integral_constant;
-        const auto go = [&](auto ns, auto ragged) {
-            gated_scan_one_token<T, ns(), ragged()><<<dim3((unsigned)(B * s.column_blocks)), dim3(256), 0, stream>>>(s);
+        const auto go = [&](auto lanes, auto groups, auto ragged) {
+            s.column_blocks = (int)ceil_div(K, 256 / lanes());
+            gated_scan_one_token<T, lanes(), groups(), ragged()><<<dim3((unsigned)(B * s.column_blocks)), dim3(256), 0, stream>>>(s);
             return check_launch("gated_scan_one_token");
         };
-        const auto with = [&](auto ns) { return N == 4 * ns() ? go(ns, std::false_type{}) : go(ns, std::true_type{}); };
-        switch (states_per_lane(N)) {
-            case 1: return with(integral_constant<int, 1>{});
-            case 2: return with(integral_constant<int, 2>{});
-            case 4: return with(integral_constant<int, 4>{});
-            case 8: return with(integral_constant<int, 8>{});
-            default: return with(integral_constant<int, 16>{});
-        }
+        const auto with = [&](auto lanes, auto groups) { return N == 4 * lanes() * groups() ? go(lanes, groups, std::false_type{}) : go(lanes, groups, std::true_type{}); };
+        constexpr integral_constant<int, 1> one{};
+        constexpr integral_constant<int, 2> two{};
+        constexpr integral_constant<int, 4> four{};
+        if (N <= 4) return with(one, one);
+        if (N <= 8) return with(two, one);
+        if (N <= 16) return with(four, one);
+        if (N <= 32) return with(four, two);
+        if (N <= 48) return with(four, integral_constant<int, 3>{});
+        return with(four, four);
     });
 }
 
