@@ -37,7 +37,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
         load_channel<NS, RAGGED>(p.a, kc + c, n0, p.N, mine, a2[c]);
         sum_d[c] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NS; i++) a2[c][i] *= kLog2e, h[c][i] = 0.0f;
+        for (int i = 0; i < NS; i++) a2[c][i] = rate_of(a2[c][i]), h[c][i] = 0.0f;
         if constexpr (!STATES_ONLY) {
             if (p.joined && chunk > 0)
                 load_channel<NS, RAGGED>(p.chunk_state, ((int64_t)(chunk - 1) * p.B + b) * p.K + kc + c, n0, p.N, mine, h[c]);
@@ -184,7 +184,11 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(RAGGED && si
     };
     load_states_of(p.a, kc, a2);
 #pragma unroll
-    for (int m = 0; m < 4; m++) a2[m] *= kLog2e, h[m] = 0.0f;
+    for (int m = 0; m < 4; m++) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) a2[m][i] = rate_of(a2[m][i]);
+        h[m] = 0.0f;
+    }
     if (p.state) load_states_of(p.state, (int64_t)b * p.K + kc, h);
     const int vt = lane / S::kAcross, vk = (lane % S::kAcross) * V, k = cb * 64 + vk, nk = max(0, min(V, p.K - k));
     bias[lane] = p.dt_bias && kc < p.K ? p.dt_bias[kc] : 0.0f;
@@ -289,7 +293,7 @@ __global__ __launch_bounds__(kShortTiles * 64) void gated_scan_short(ScanArgs<T>
     const int n = lane & 15, cl = lane >> 4, kc = cb * kShortChannels + cl;
     const bool mine = !RAGGED || (kc < p.K && n < p.N);
     const int64_t state = (int64_t)kc * p.N + n;
-    const float a2 = mine ? p.a[state] * kLog2e : 0.0f;
+    const float a2 = mine ? rate_of(p.a[state]) : 0.0f;
     const float start = mine && p.state ? p.state[(int64_t)b * p.K * p.N + state] : 0.0f;
 
     const float D_in = softplus_of(x + bias);
@@ -359,7 +363,7 @@ __global__ __launch_bounds__(256) void gated_scan_one_token(ScanArgs<T> p) {
     for (int j = 0; j < GROUPS; j++) {
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            h[j][i] = fmaf(__builtin_amdgcn_exp2f(a[j][i] * kLog2e * D), h[j][i], Du * (float)B[j][i]);
+            h[j][i] = fmaf(__builtin_amdgcn_exp2f(rate_of(a[j][i]) * D), h[j][i], Du * (float)B[j][i]);
             v = i < n[j] ? fmaf(h[j][i], (float)CC[j][i], v) : v;
         }
         store_first<4>(p.state_out + at + j * LANES * 4, n[j], h[j]);

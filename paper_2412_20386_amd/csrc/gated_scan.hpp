@@ -42,6 +42,13 @@ struct ScanLane {
 };
 
 constexpr float kLog2e = 1.44269504088896340736f;
+// a log2(e), so that e^{D a} = 2^{D rate}.  Not below the lowest number: what is staged behind the last token and joined behind the last chunk changes
+// nothing because its D is 0, and 0 times minus infinity would be NaN (so would minus infinity times a gradient of 0).  2^{D rate} is 0 either
+// way, for every D from 1e-36 on.
+__device__ __forceinline__ float rate_of(float a) {
+    const float rate = a * kLog2e;
+    return rate < -3.402823466e38f ? -3.402823466e38f : rate;  // (a NaN stays one)
+}
 
 // States of a quad's lane: the power of two that has room for N
 inline int states_per_lane(int64_t N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
@@ -169,7 +176,7 @@ __global__ __launch_bounds__(kJoinStates *kJoinRuns) void join_chunks(float *__r
     const int64_t channel = there ? at / N : 0;
     const int steps = chunks - 1;                                    // chunks that leave something to another one
     const int length = join_length(steps), first = run * length;
-    const float a2 = there ? a[channel % K * N + (at - channel * N)] * kLog2e : 0.0f;
+    const float a2 = there ? rate_of(a[channel % K * N + (at - channel * N)]) : 0.0f;
     float end[kJoinRun], D[kJoinRun], h = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kJoinRun; i++) {

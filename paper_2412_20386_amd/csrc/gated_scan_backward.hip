@@ -47,7 +47,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
         load_channel<NS, RAGGED>(p.a, kc + c, n0, p.N, mine, a2[c]);
         sum_d[c] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NS; i++) a2[c][i] *= kLog2e, carry[c][i] = da[c][i] = 0.0f;
+        for (int i = 0; i < NS; i++) a2[c][i] = rate_of(a2[c][i]), carry[c][i] = da[c][i] = 0.0f;
         if constexpr (!CARRY_ONLY) {
             if (p.joined) {
                 if (chunk + 1 < p.chunks) load_channel<NS, RAGGED>(p.chunk_state, ((int64_t)(chunk + 1) * p.B + b) * p.K + kc + c, n0, p.N, mine, carry[c]);
