@@ -6,10 +6,16 @@ the logarithm of 1 + e^-|x| (6), D is off by (8 + 3 |x|) U of itself; a decay e^
 (3), of a sum over the S tokens of a chunk (S, and 16 runs) where it is taken for all of them together, and 2 for the instruction.  A state then takes over
 the error of the one before times the decay, and adds those of the decay, of D u b (2) and of its own sum.  `magnitude` values have every
 term's absolute value: they bound the states that a chunk reaches from zero too.
+
+Below 2^-126 a rounding is no part of the value: the smallest step is 2^-149, so that each rounding there is off by up to 2^-150 (TINY), and a decay
+below 2^-126 (FLUSHED) comes from the instruction as 0.  Both are added as they are, for every product and every sum: 3 a token to a state (the product D u b, the
+multiply-add, the join's second product), 2 a term to a sum of products, and a few to what is made of the sums.
 """
 import torch
 
 from token_ops_ref import U, sigmoid, softplus
+
+TINY, FLUSHED = 2.0 ** -150, 2.0 ** -126
 
 
 def bounds(dy, u, dt, a, b, c, d, z, dt_bias, state=None, chunk=160):
@@ -38,13 +44,13 @@ def bounds(dy, u, dt, a, b, c, d, z, dt_bias, state=None, chunk=160):
         A, e_A = decay(t)
         q = (D * u)[:, t, :, None] * b[:, t, None, :]
         h[t + 1], m[t + 1] = A * h[t] + q, A * m[t] + q.abs()
-        e_h[t + 1] = A * e_h[t] + e_A * A * m[t] + (e_D[:, t, :, None] + 2 * U) * q.abs() + U * m[t + 1]
+        e_h[t + 1] = A * e_h[t] + (e_A * A + FLUSHED) * m[t] + (e_D[:, t, :, None] + 2 * U) * q.abs() + U * m[t + 1] + 3 * TINY
         C = c[:, t, None, :]
         s[:, t] = (C * h[t + 1]).sum(-1) + skip * u[:, t]
         size = (C.abs() * m[t + 1]).sum(-1)
         s_size[:, t] = size + (skip * u[:, t]).abs()
-        e_s[:, t] = (C.abs() * e_h[t + 1]).sum(-1) + (N + 2) * U * size + U * s_size[:, t]
-    out = dict(y=(s * gate, e_s * gate.abs() + (e_gate + U) * s_size * gate.abs()), state_out=(h[L], e_h[L]), marks=(h[:L:8], e_h[:L:8]))
+        e_s[:, t] = (C.abs() * e_h[t + 1]).sum(-1) + (N + 2) * U * size + U * s_size[:, t] + (2 * N + 4) * TINY
+    out = dict(y=(s * gate, e_s * gate.abs() + (e_gate + U) * s_size * gate.abs() + 3 * TINY), state_out=(h[L], e_h[L]), marks=(h[:L:8], e_h[:L:8]))
 
     G, e_G = dy * gate, e_gate + U
     du, ddt, e_du, e_ddt, size_ddt = (new(B, L, K) for _ in range(5))
@@ -57,32 +63,32 @@ def bounds(dy, u, dt, a, b, c, d, z, dt_bias, state=None, chunk=160):
         e_Gt, e_Dt = e_G[:, t, :, None], e_D[:, t, :, None]
         cg = C * Gt
         g, m_g = cg + carry, cg.abs() + m_carry
-        e_g = cg.abs() * e_Gt + e_carry + U * m_g
-        carry, m_carry, e_carry = A * g, A * m_g, A * e_g + e_A * A * m_g
+        e_g = cg.abs() * e_Gt + e_carry + U * m_g + 2 * TINY
+        carry, m_carry, e_carry = A * g, A * m_g, A * e_g + (e_A * A + FLUSHED) * m_g + 2 * TINY
         w, m_w = carry * h[t], m_carry * m[t]
-        e_w = e_carry * m[t] + m_carry * e_h[t] + U * m_w
+        e_w = e_carry * m[t] + m_carry * e_h[t] + U * m_w + TINY
         db[:, t], dc[:, t] = (g * Du).sum(1), (h[t + 1] * Gt).sum(1)
-        e_db[:, t] = (e_g * Du.abs() + m_g * Du.abs() * (e_Dt + U + by_k)).sum(1)
-        e_dc[:, t] = (e_h[t + 1] * Gt.abs() + m[t + 1] * Gt.abs() * (e_Gt + by_k)).sum(1)
+        e_db[:, t] = (e_g * Du.abs() + m_g * Du.abs() * (e_Dt + U + by_k)).sum(1) + 2 * K * TINY
+        e_dc[:, t] = (e_h[t + 1] * Gt.abs() + m[t + 1] * Gt.abs() * (e_Gt + by_k)).sum(1) + 2 * K * TINY
         gb, m_gb, wa, m_wa = (g * Bt).sum(-1), (m_g * Bt.abs()).sum(-1), (w * a).sum(-1), (m_w * a.abs()).sum(-1)
-        e_gb, e_wa = (e_g * Bt.abs()).sum(-1) + (N + 2) * U * m_gb, (e_w * a.abs()).sum(-1) + (N + 6) * U * m_wa
+        e_gb, e_wa = (e_g * Bt.abs()).sum(-1) + (N + 2) * U * m_gb + 2 * N * TINY, (e_w * a.abs()).sum(-1) + (N + 6) * U * m_wa + 2 * N * TINY
         dG = skip * G[:, t]
         du[:, t] = dG + D[:, t] * gb
-        e_du[:, t] = dG.abs() * (e_G[:, t] + 2 * U) + D[:, t] * (e_gb + m_gb * (e_D[:, t] + 3 * U))
+        e_du[:, t] = dG.abs() * (e_G[:, t] + 2 * U) + D[:, t] * (e_gb + m_gb * (e_D[:, t] + 3 * U)) + 4 * TINY
         sig = sigmoid(x[:, t])
         ddt[:, t] = (u[:, t] * gb + wa) * sig
         size_ddt[:, t] = (u[:, t].abs() * m_gb + m_wa) * sig
-        e_ddt[:, t] = (u[:, t].abs() * e_gb + e_wa) * sig + size_ddt[:, t] * (e_sig[:, t] + 4 * U)
+        e_ddt[:, t] = (u[:, t].abs() * e_gb + e_wa) * sig + size_ddt[:, t] * (e_sig[:, t] + 4 * U) + 4 * TINY
         da += (w * D[:, t, :, None]).sum(0)
-        e_da += (e_w * D[:, t, :, None] + m_w * D[:, t, :, None] * (e_Dt + U + by_t)).sum(0)
+        e_da += (e_w * D[:, t, :, None] + m_w * D[:, t, :, None] * (e_Dt + U + by_t)).sum(0) + 2 * B * TINY
     out |= dict(du=(du, e_du), ddt=(ddt, e_ddt), da=(da, e_da), db=(db, e_db), dc=(dc, e_dc))
-    out["dd"] = None if d is None else ((G * u).sum((0, 1)), ((G * u).abs() * (e_G + U + by_t)).sum((0, 1)))
+    out["dd"] = None if d is None else ((G * u).sum((0, 1)), ((G * u).abs() * (e_G + U + by_t)).sum((0, 1)) + 2 * B * L * TINY)
     if z is None:
         out["dz"] = None
     else:
         f = sigmoid(z)
         size = f + (z * f * (1 - f)).abs()  # (its two terms cancel near z = -1.28)
-        out["dz"] = dy * s * (f + z * f * (1 - f)), dy.abs() * size * (e_s + s_size * (6 * z.abs() + 14) * U)
+        out["dz"] = dy * s * (f + z * f * (1 - f)), dy.abs() * size * (e_s + s_size * (6 * z.abs() + 14) * U) + 6 * TINY
     out["ddt_bias"] = None if dt_bias is None else (ddt.sum((0, 1)), (e_ddt + size_ddt * by_t).sum((0, 1)))
     return out
 

@@ -78,3 +78,23 @@ def test_states_that_keep_nothing_step_by_step(B, K, N, dtype):
     exact["a"] = exact["a"].clamp(min=-1e300)
     want = bounds(torch.zeros_like(exact["u"]), **exact, state=state.to(DEV).double())
     assert within(_time(y, B, 1, False), *want["y"], TYPES[dtype]) <= 1 and within(now, *want["state_out"], torch.float32) <= 1
+
+
+@pytest.mark.parametrize("with_state", [False, True])
+@pytest.mark.parametrize("L,N,reverse", [(100, 17, False), (600, 16, True), (200, 16, False), (200, 3, True), (333, 64, False)])
+def test_states_that_grow_over_a_chunk(L, N, reverse, with_state):
+    """A state grows by e^100, beyond the range of fp32, over 16 tokens, where it and the gradients are small or zero: its values are finite, and so
+    are those of sequences in chunks, whose decays over a chunk are one number."""
+    B, K = 1, 20
+    print("growth", L, N, reverse, with_state, flush=True)
+    v, _ = _scan_inputs(L + N, B, L, K, N, "f32", bias=False)
+    v["dt"] = v["dt"] * 0.5 - 7  # steps of about 0.001
+    v["dt"][32:48], v["u"][:64] = 100 / 16, 0.0  # (softplus(6.25) = 6.252)
+    v["a"][:, N // 2] = 1.0
+    state = torch.full((B, K, N), 1e-35) if with_state else None
+    dy = Draw(5)(L, K) * 1e-30
+    if reverse:  # the same in the order of time
+        for k in BY_TOKEN:
+            v[k] = v[k].flip(0).contiguous()
+        dy = dy.flip(0).contiguous()
+    _check(v, state, dy, B, L, reverse, torch.float32)
