@@ -55,7 +55,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
                 for (int s = 0; s < kJoin - 2; s++)
                     if ((uint32_t)s < chunk)
 #pragma unroll
-                        for (int j = 0; j < NS; j++) h[c][j] = decayed(h[c][j], a2[c][j] * D[s]) + end[s][j];
+                        for (int j = 0; j < NS; j++) h[c][j] = decayed(h[c][j], a2[c][j] * D[s], end[s][j]);
             }
         }
     }
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(kShortTiles * 64) void gated_scan_short(ScanArgs<T>
     if (n == 0) tile.sum_d[cl] = sum;
     __syncthreads();
     h = start;
-    for (int s = 0; s < (int)(threadIdx.x >> 6); s++) h = decayed(h, a2 * tiles[s].sum_d[cl]) + tiles[s].end[cl][n];
+    for (int s = 0; s < (int)(threadIdx.x >> 6); s++) h = decayed(h, a2 * tiles[s].sum_d[cl], tiles[s].end[cl][n]);
 #pragma unroll
     for (int t = 0; t < kTile; t++) {
         if (p.marks && t % kMark == 0 && t <= last && mine) p.marks[((t0 + t) / kMark * p.B + b) * p.K * p.N + state] = h;

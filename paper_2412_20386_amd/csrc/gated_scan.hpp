@@ -50,12 +50,11 @@ __device__ __forceinline__ float rate_of(float a) {
     return rate < -3.402823466e38f ? -3.402823466e38f : rate;  // (a NaN stays one)
 }
 
-// 2^x h for the decay over a whole chunk: with a rate above 0 it leaves the range of fp32 where h is 0 or small and the product does not, so the whole
-// powers of two come last.  (The factor before them is at most 1; beyond 300 the result is 0 or infinite for every h but 0.)
-__device__ __forceinline__ float decayed(float h, float x) {
-    x = fminf(fmaxf(x, -300.0f), 300.0f);
-    const float whole = ceilf(x);
-    return __builtin_amdgcn_ldexpf(h * __builtin_amdgcn_exp2f(x - whole), (int)whole);
+// 2^x h + end, for the decay over a whole chunk: with a rate above 0 it leaves the range of fp32 where h is 0 or small and the product does not, so
+// it is multiplied in as its square root, twice.  (Where x is above 254, h has to be subnormal for the product to be a number.)
+__device__ __forceinline__ float decayed(float h, float x, float end) {
+    const float root = __builtin_amdgcn_exp2f(fminf(0.5f * x, 127.0f));
+    return fmaf(h * root, root, end);
 }
 
 // States of a quad's lane: the power of two that has room for N
@@ -195,16 +194,16 @@ __global__ __launch_bounds__(kJoinStates *kJoinRuns) void join_chunks(float *__r
     }
 #pragma unroll
     for (int i = 0; i < kJoinRun; i++) {
-        h = decayed(h, a2 * D[i]) + end[i];
+        h = decayed(h, a2 * D[i], end[i]);
         sum += D[i];
     }
     ends[run][s] = h, sums[run][s] = sum;
     __syncthreads();
     h = !BACKWARD && state && there ? state[at] : 0.0f;
-    for (int r = 0; r < run; r++) h = decayed(h, a2 * sums[r][s]) + ends[r][s];
+    for (int r = 0; r < run; r++) h = decayed(h, a2 * sums[r][s], ends[r][s]);
 #pragma unroll
     for (int i = 0; i < kJoinRun; i++) {
-        h = decayed(h, a2 * D[i]) + end[i];
+        h = decayed(h, a2 * D[i], end[i]);
         if (there && i < length && first + i < steps) chunk_state[(BACKWARD ? chunks - 1 - (first + i) : first + i) * channels * N + at] = h;
     }
 }

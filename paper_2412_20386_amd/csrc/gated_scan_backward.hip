@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(NS * C > 8 ?
                 for (int s = 0; s < kJoin - 2; s++)
                     if ((int)p.chunks - 1 - s > (int)chunk)
 #pragma unroll
-                        for (int j = 0; j < NS; j++) carry[c][j] = decayed(carry[c][j], a2[c][j] * D[s]) + end[s][j];
+                        for (int j = 0; j < NS; j++) carry[c][j] = decayed(carry[c][j], a2[c][j] * D[s], end[s][j]);
             }
         }
     }
