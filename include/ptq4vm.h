@@ -47,7 +47,8 @@ typedef enum {
     PTQ4VM_ERR_STRIDE = -3, /* a leading dimension is smaller than the row width */
     PTQ4VM_ERR_ALIGN = -4,  /* a base pointer is not aligned as stated above */
     PTQ4VM_ERR_HIP = -5,    /* the HIP runtime refused a launch; see ptq4vm_last_hip_error() */
-    PTQ4VM_ERR_VALUE = -6   /* ptq4vm_validate_scales found a scale that is not a finite number > 0 */
+    PTQ4VM_ERR_VALUE = -6,  /* ptq4vm_validate_scales found a scale that is not a finite number > 0 */
+    PTQ4VM_ERR_OVERLAP = -7 /* an output shares memory with an input that other workgroups still read */
 } ptq4vm_status;
 
 /* Largest K for which sum_k (+-127)(+-127) is guaranteed to fit int32: floor((2^31-1)/127^2). */
@@ -341,7 +342,7 @@ typedef enum { PTQ4VM_F16 = 0, PTQ4VM_BF16 = 1, PTQ4VM_F32 = 2 } ptq4vm_dtype;
  *   a [K, N] f32 in, dense;  d [K], dt_bias [K] f32 in, may be NULL (zeros);  z [B*L, K] T in, may be NULL (no gate: y = s)
  *   state     [B, K, N] f32 in, dense, may be NULL (zeros): h before the first token
  *   y         [B*L, K]  T out
- *   state_out [B, K, N] f32 out, may be NULL: h behind the last token.  Not the buffer of `state`.
+ *   state_out [B, K, N] f32 out, may be NULL: h behind the last token.  May not overlap `state` (PTQ4VM_ERR_OVERLAP).
  *   marks     [PTQ4VM_SCAN_MARKS(L), B, K, N] f32 out, may be NULL: h before every PTQ4VM_SCAN_TILE-th token, for the backward
  *             pass
  * Few long sequences are cut into chunks that run side by side (two launches).  Errors: NULL u / dt / a / b / c / y, sizes out of
@@ -374,7 +375,7 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
 
 /*
  * One token of each of B sequences: ptq4vm_gated_scan with L = 1 on the states [B, K, N], which it advances.  state_out may be
- * the buffer of `state` (in place).  Errors as there, and NULL state / state_out.
+ * the buffer of `state` (in place), but not overlap it otherwise.  Errors as there, and NULL state / state_out.
  */
 int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d,
                            const void *z, const float *dt_bias, const float *state, void *y, float *state_out, int64_t B,
@@ -387,9 +388,11 @@ int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float
  *   x [B*L, K] T in, w [K, W] f32 in, dense, bias [K] f32 in, may be NULL
  *   state     [B, W - 1, K] T in, dense, may be NULL (zeros): x of the W - 1 tokens before the first
  *   y         [B*L, K] T out
- *   state_out [B, W - 1, K] T out, may be NULL: x of the last W - 1 tokens (of state's where L < W - 1).  Not the buffer of `state`.
+ *   state_out [B, W - 1, K] T out, may be NULL: x of the last W - 1 tokens (of state's where L < W - 1).  May not overlap `state`.
  * The backward pass gives dx [B*L, K] T, dw [K, W] f32 and dbias [K] f32 (may be NULL) for the gradient dy of y; the state is a
  * constant.  The step is L = 1 on states that it advances; its state_out may be the buffer of `state`.
+ * A token is read again by the runs of tokens beside its own: y may share no element with x, nor dx with x or dy (PTQ4VM_ERR_OVERLAP;
+ * halves of one wider matrix share none).  Where L = 1, y may be x itself, and dx x or dy.
  * Errors: NULL x / w / y (dy / x / w / dx / dw; x / w / state / y / state_out), sizes out of range, ld* < K, misalignment,
  * workspace too small (PTQ4VM_ERR_SHAPE) or missing.  B = 0 writes zeros to dw and dbias.
  */

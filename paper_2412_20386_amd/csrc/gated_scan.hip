@@ -435,6 +435,7 @@ int ptq4vm_gated_scan(int dtype, const void *u, const void *dt, const float *a, 
     if (workspace_bytes < need) return PTQ4VM_ERR_SHAPE;
     if (!aligned_to(state, 4) || !aligned_to(state_out, 4) || !aligned_to(marks, 4) || !aligned_to(workspace, 16)) return PTQ4VM_ERR_ALIGN;
     if (B == 0) return PTQ4VM_OK;
+    if (overlap(state, state_out, B * K * N * 4)) return PTQ4VM_ERR_OVERLAP;  // (the chunks of a sequence read it in their own time)
     const ScanPlan plan = forward_plan(B, L, K, N);
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     return for_dtype(dtype, [&](auto zero) {
@@ -485,6 +486,7 @@ int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float
     if (!aligned_to(state, 4) || !aligned_to(state_out, 4)) return PTQ4VM_ERR_ALIGN;
     if (!grid_fits(B * ceil_div(K, 64), 256)) return PTQ4VM_ERR_SHAPE;
     if (B == 0) return PTQ4VM_OK;
+    if (state != state_out && overlap(state, state_out, B * K * N * 4)) return PTQ4VM_ERR_OVERLAP;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     return for_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);

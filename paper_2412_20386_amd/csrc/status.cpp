@@ -25,6 +25,7 @@ const char *ptq4vm_status_string(int status) {
         case PTQ4VM_ERR_ALIGN: return "misaligned base pointer";
         case PTQ4VM_ERR_HIP: return "HIP runtime error";
         case PTQ4VM_ERR_VALUE: return "a scale is not a finite number greater than zero";
+        case PTQ4VM_ERR_OVERLAP: return "an output overlaps an input that is still read";
         default: return "unknown status";
     }
 }

@@ -23,7 +23,7 @@ template <typename T>
 struct ConvArgs {
     Tokens<T> x, y, dy;  // (y: dx in the backward pass)
     const float *w, *bias;
-    const T *state;  // may be the buffer of state_out where one run spans the sequence
+    const T *state;  // may be the buffer of state_out for one token
     T *state_out;
     float *partial;
     int K, B, silu;
@@ -262,6 +262,14 @@ int check_conv(int dtype, const void *x, const float *w, const float *bias, cons
     return PTQ4VM_OK;
 }
 
+// Whether the lanes of one run would write what those of another read: an output's elements among an input's.  A sequence of one token is
+// read by the lanes that write it, so there the two may be the same.
+bool run_overlap(int dtype, const void *out, int64_t ld_out, const void *in, int64_t ld_in, int64_t B, int64_t L, int64_t K) {
+    const int64_t e = (int64_t)dtype_bytes(dtype), rows = B * L;
+    if (L == 1 && out == in && (rows == 1 || ld_out == ld_in)) return false;
+    return overlap(out, ld_out * e, in, ld_in * e, rows, K * e);
+}
+
 // f(W, WHOLE)
 template <typename F>
 int for_filter(int64_t W, bool whole, F &&f) {
@@ -320,6 +328,7 @@ int ptq4vm_token_conv(int dtype, const void *x, const float *w, const float *bia
     if (B != 0 && !y) return PTQ4VM_ERR_NULL;
     if (ldx < K || ldy < K) return PTQ4VM_ERR_STRIDE;
     if (!aligned_to(y, dtype_bytes(dtype)) || !aligned_to(state_out, dtype_bytes(dtype))) return PTQ4VM_ERR_ALIGN;
+    if (B > 0 && (run_overlap(dtype, y, ldy, x, ldx, B, L, K) || overlap(state, state_out, B * (W - 1) * K * (int64_t)dtype_bytes(dtype)))) return PTQ4VM_ERR_OVERLAP;
     return conv(dtype, x, w, bias, state, y, state_out, silu, reverse, B, L, K, W, ldx, ldy, stream);
 }
 
@@ -330,6 +339,8 @@ int ptq4vm_token_conv_step(int dtype, const void *x, const float *w, const float
     if (B != 0 && (!state || !y || !state_out)) return PTQ4VM_ERR_NULL;
     if (ldx < K || ldy < K) return PTQ4VM_ERR_STRIDE;
     if (!aligned_to(y, dtype_bytes(dtype)) || !aligned_to(state_out, dtype_bytes(dtype))) return PTQ4VM_ERR_ALIGN;
+    if (B > 0 && (run_overlap(dtype, y, ldy, x, ldx, B, 1, K) || (state != state_out && overlap(state, state_out, B * (W - 1) * K * (int64_t)dtype_bytes(dtype)))))
+        return PTQ4VM_ERR_OVERLAP;
     return conv(dtype, x, w, bias, state, y, state_out, silu, 0, B, 1, K, W, ldx, ldy, stream);
 }
 
@@ -350,6 +361,7 @@ int ptq4vm_token_conv_backward(int dtype, const void *dy, const void *x, const f
     if (workspace_bytes < ptq4vm_token_conv_backward_workspace(B, L, K, W)) return PTQ4VM_ERR_SHAPE;
     const uintptr_t e = dtype_bytes(dtype);
     if (!aligned_to(dy, e) || !aligned_to(dx, e) || !aligned_to(dw, 4) || !aligned_to(dbias, 4) || !aligned_to(workspace, 16)) return PTQ4VM_ERR_ALIGN;
+    if (B > 0 && (run_overlap(dtype, dx, lddx, x, ldx, B, L, K) || run_overlap(dtype, dx, lddx, dy, lddy, B, L, K))) return PTQ4VM_ERR_OVERLAP;
     hipStream_t stream = static_cast<hipStream_t>(stream_);
     int64_t groups = 0;
     if (B > 0) {

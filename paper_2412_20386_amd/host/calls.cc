@@ -837,9 +837,9 @@ PyMethodDef methods[] = {
     FAST(gated_scan_step, "gated_scan_step(u, dt, a, b, c, d, z, dt_bias, state, y=None, state_out=None)\n--\n\n"
                           "ptq4vm_gated_scan_step: y [B, K] for one token of each sequence; state (f32 [B, K, N]) advances in place unless state_out is given."),
     FAST(token_conv, "token_conv(x, w, bias, B, L, silu=True, reverse=False, state=None, y=None, state_out=None)\n--\n\n"
-                     "ptq4vm_token_conv: y [B*L, K] of x's type; state_out ([B, W - 1, K] of x's type, not state itself) is filled if given."),
+                     "ptq4vm_token_conv: y [B*L, K] of x's type, apart from x; state_out ([B, W - 1, K] of x's type, not state itself) is filled if given."),
     FAST(token_conv_backward, "token_conv_backward(dy, x, w, bias, B, L, silu=True, reverse=False, state=None, dx=None)\n--\n\n"
-                              "ptq4vm_token_conv_backward: (dx, dw, dbias); dbias is None without a bias."),
+                              "ptq4vm_token_conv_backward: (dx, dw, dbias); dx is apart from x and dy, dbias None without a bias."),
     FAST(token_conv_step, "token_conv_step(x, w, bias, state, silu=True, y=None, state_out=None)\n--\n\n"
                           "ptq4vm_token_conv_step: y [B, K] for one token of each sequence; state ([B, W - 1, K]) advances in place unless state_out is given."),
     FAST(residual_norm, "residual_norm(h, residual, w, gate=None, w_post=None, scale=1.0, eps=1e-5, y=None, residual_out=None)\n--\n\n"
