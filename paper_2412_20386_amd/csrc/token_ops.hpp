@@ -166,10 +166,15 @@ __device__ __forceinline__ void sum_columns(const float *__restrict__ partial, i
     }
 }
 __global__ __launch_bounds__(kSumThreads) void sum_partials(const float *__restrict__ partial, int64_t rows, int64_t cols, SumOut out) {
-    sum_columns(partial, rows, cols, cols, out, blockIdx.x);
+    for (uint32_t block = blockIdx.x; (int64_t)block * kSumCols < cols; block += gridDim.x) {
+        sum_columns(partial, rows, cols, cols, out, block);
+        __syncthreads();  // (the next columns go through the same LDS)
+    }
 }
+constexpr int64_t kSumBlocks = (int64_t)1 << 21;  // 2^31 threads: a grid holds fewer than 2^32
 inline int launch_sum_partials(const float *partial, int64_t rows, int64_t cols, const SumOut &out, hipStream_t stream) {
-    sum_partials<<<dim3((unsigned)ceil_div(cols, kSumCols)), dim3(kSumThreads), 0, stream>>>(partial, rows, cols, out);
+    const int64_t blocks = ceil_div(cols, kSumCols);
+    sum_partials<<<dim3((unsigned)(blocks < kSumBlocks ? blocks : kSumBlocks)), dim3(kSumThreads), 0, stream>>>(partial, rows, cols, out);
     return check_launch("sum_partials");
 }
 }  // namespace
