@@ -328,8 +328,10 @@ int ptq4vm_f16_linear(const void *x_f16, const void *w_f16, const void *bias_f16
  * pointers need only be aligned to an element, and nothing beyond a row's width is read or written.  Gradients of parameters
  * are summed in a fixed order: the same inputs give the same bits.  `reverse` != 0 lets time run from a sequence's last row to
  * its first (a block that scans its tokens both ways): the state before the first token is then the one behind the last row.
- * At most 2^31 - 1 rows.  Workspaces are device scratch of the caller, 16-byte aligned, of at least the bytes that the
- * _workspace function says (0: may be NULL); their contents need no initialisation and are free once the call's work is done.
+ * At most 2^31 - 1 rows; each operator names its other limits.  Gradients come from the _backward calls alone: a forward call
+ * records nothing but what it is asked to leave.  Workspaces are device scratch of the caller, 16-byte aligned, of at least the
+ * bytes that the _workspace function says (0: may be NULL); their contents need no initialisation and are free once the call's
+ * work is done.
  */
 typedef enum { PTQ4VM_F16 = 0, PTQ4VM_BF16 = 1, PTQ4VM_F32 = 2 } ptq4vm_dtype;
 
@@ -345,8 +347,10 @@ typedef enum { PTQ4VM_F16 = 0, PTQ4VM_BF16 = 1, PTQ4VM_F32 = 2 } ptq4vm_dtype;
  *   state_out [B, K, N] f32 out, may be NULL: h behind the last token.  May not overlap `state` (PTQ4VM_ERR_OVERLAP).
  *   marks     [PTQ4VM_SCAN_MARKS(L), B, K, N] f32 out, may be NULL: h before every PTQ4VM_SCAN_TILE-th token, for the backward
  *             pass
- * Few long sequences are cut into chunks that run side by side (two launches).  Errors: NULL u / dt / a / b / c / y, sizes out of
- * range (N up to PTQ4VM_MAX_SCAN_N), ld* below a row's width, misalignment, workspace too small (PTQ4VM_ERR_SHAPE) or missing.
+ * Few long sequences are cut into chunks that run side by side (two launches, three from nine chunks on).  Decays below 2^-126 are 0;
+ * a may be minus infinity (nothing is kept).  Errors: NULL u / dt / a / b / c / y, sizes out of range (N up to PTQ4VM_MAX_SCAN_N, K up to
+ * 2^23 - 1, B ceil(K / 16) below 2^25), ld* below a row's width or of 2^26 and more (PTQ4VM_ERR_STRIDE), misalignment, workspace
+ * too small (PTQ4VM_ERR_SHAPE) or missing.
  */
 #define PTQ4VM_SCAN_TILE 8
 #define PTQ4VM_SCAN_MARKS(L) ((((int64_t)(L)) + PTQ4VM_SCAN_TILE - 1) / PTQ4VM_SCAN_TILE)
@@ -375,7 +379,8 @@ int ptq4vm_gated_scan_backward(int dtype, const void *dy, const void *u, const v
 
 /*
  * One token of each of B sequences: ptq4vm_gated_scan with L = 1 on the states [B, K, N], which it advances.  state_out may be
- * the buffer of `state` (in place), but not overlap it otherwise.  Errors as there, and NULL state / state_out.
+ * the buffer of `state` (in place), but not overlap it otherwise.  Errors as there, NULL state / state_out, and
+ * B ceil(K / 64) of 2^24 and more (PTQ4VM_ERR_SHAPE).
  */
 int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float *a, const void *b, const void *c, const float *d,
                            const void *z, const float *dt_bias, const float *state, void *y, float *state_out, int64_t B,
@@ -393,8 +398,9 @@ int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float
  * constant.  The step is L = 1 on states that it advances; its state_out may be the buffer of `state`.
  * A token is read again by the runs of tokens beside its own: y may share no element with x, nor dx with x or dy (PTQ4VM_ERR_OVERLAP;
  * halves of one wider matrix share none).  Where L = 1, y may be x itself, and dx x or dy.
- * Errors: NULL x / w / y (dy / x / w / dx / dw; x / w / state / y / state_out), sizes out of range, ld* < K, misalignment,
- * workspace too small (PTQ4VM_ERR_SHAPE) or missing.  B = 0 writes zeros to dw and dbias.
+ * Errors: NULL x / w / y (dy / x / w / dx / dw; x / w / state / y / state_out), sizes out of range (K up to 2^27 - 1, and for y fewer than
+ * 2^32 lanes: one for 8 channels of 4 to 16 tokens), ld* < K, misalignment, workspace too small (PTQ4VM_ERR_SHAPE) or missing.
+ * B = 0 writes zeros to dw and dbias.
  */
 int ptq4vm_token_conv(int dtype, const void *x, const float *w, const float *bias, const void *state, void *y, void *state_out,
                       int silu, int reverse, int64_t B, int64_t L, int64_t K, int64_t W, int64_t ldx, int64_t ldy, void *stream);
@@ -413,7 +419,7 @@ int ptq4vm_token_conv_step(int dtype, const void *x, const float *w, const float
  *   w [K], w_post [K] f32 in; w_post may be NULL (no norm after the block)
  *   gate     [G, K] f32 in, dense, may be NULL (ones): row i takes gate row i / (M / G), so G = 1 is a gate per channel, G = B one
  *            per image, G = M one per token
- * y is computed from r before it is rounded to stream_dtype.  The backward pass takes h and r, the gradient dy of y and the
+ * y is computed from r before it is rounded to stream_dtype.  Sums of squares are fp32: where a row's pass 3.4e38, norm(v) is 0.  The backward pass takes h and r, the gradient dy of y and the
  * gradient dr of r from the blocks behind (may be NULL: zeros) and gives dh [M, K] T, dresidual [M, K] stream_dtype (may be NULL),
  * dw [K], dgate [G, K] and dw_post [K] f32.
  * Errors: NULL h / w / y / r (dy / h / r / w / dh / dw, and dgate, dw_post with their inputs), sizes out of range (K up to

@@ -60,9 +60,11 @@ __device__ __forceinline__ float decayed(float h, float x, float end) {
 // States of a quad's lane: the power of two that has room for N
 inline int states_per_lane(int64_t N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 
-// How a problem is cut: one chunk of tokens per sequence unless the device would be half empty, then chunks for `held` wavefronts,
-// of 32 tokens at least and whole tiles; two channels to a lane (fewer instructions for each) where that still leaves `full` wavefronts;
-// not at the price of chunks if `whole`.
+// How a problem is cut: one chunk of tokens per sequence from 1024 wavefronts on, else chunks for `held` wavefronts, but no more of them than
+// one for every 32 tokens begun (so of 17 at least), of whole tiles; two channels to a lane (fewer instructions for each) where that still
+// leaves `full` wavefronts; not at the price of chunks if `whole`.  Above 16 states there is one channel to a lane only.  Whole and in chunks, us,
+// forward / backward: 16 x 4000 x 1024 x 32 (1024 wavefronts) 756 / 3604 and 791 / 2199, with 64 states 1153 / 4460 and 1248 / 5021; 24 x 2000 x
+// 1024 x 32 518 / 1881 and 534 / 1623; 31 sequences of them 514 / 1917 and 651 / 2149; 64 x 197 x 512 x 32 56 / 200 and 84 / 248.
 // From kJoin chunks on, a kernel of its own runs through them; up to there each wavefront does, all loads in flight.
 constexpr int kMostChunks = 256, kJoin = 9;
 struct ScanPlan {

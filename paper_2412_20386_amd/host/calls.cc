@@ -831,19 +831,22 @@ PyMethodDef methods[] = {
     FAST(f16_linear, "f16_linear(x, w, bias, y=None)\n--\n\nptq4vm_f16_linear: y fp16 [M, N]."),
     FAST(gated_scan, "gated_scan(u, dt, a, b, c, d, z, dt_bias, B, L, reverse=False, state=None, y=None, state_out=None, marks=None)\n--\n\n"
                      "ptq4vm_gated_scan: y [B*L, K] of u's type (fp16, bfloat16, fp32); state_out (f32 [B, K, N], not state itself) and marks\n"
-                     "(f32 [scan_marks(L), B, K, N], for the backward pass) are filled if given."),
+                     "(f32 [scan_marks(L), B, K, N], for the backward pass) are filled if given.  Records nothing for autograd: gradients come from\n"
+                     "gated_scan_backward, called with the same arguments."),
     FAST(gated_scan_backward, "gated_scan_backward(dy, u, dt, a, b, c, d, z, dt_bias, marks, B, L, reverse=False, du=None, ddt=None, db=None, dc=None, dz=None)\n--\n\n"
                               "ptq4vm_gated_scan_backward: (du, ddt, da, db, dc, dd, dz, ddt_bias); None for the gradient of an input that is None."),
     FAST(gated_scan_step, "gated_scan_step(u, dt, a, b, c, d, z, dt_bias, state, y=None, state_out=None)\n--\n\n"
                           "ptq4vm_gated_scan_step: y [B, K] for one token of each sequence; state (f32 [B, K, N]) advances in place unless state_out is given."),
     FAST(token_conv, "token_conv(x, w, bias, B, L, silu=True, reverse=False, state=None, y=None, state_out=None)\n--\n\n"
-                     "ptq4vm_token_conv: y [B*L, K] of x's type, apart from x; state_out ([B, W - 1, K] of x's type, not state itself) is filled if given."),
+                     "ptq4vm_token_conv: y [B*L, K] of x's type, apart from x; state_out ([B, W - 1, K] of x's type, not state itself) is filled if given.\n"
+                     "Records nothing for autograd: gradients come from token_conv_backward."),
     FAST(token_conv_backward, "token_conv_backward(dy, x, w, bias, B, L, silu=True, reverse=False, state=None, dx=None)\n--\n\n"
                               "ptq4vm_token_conv_backward: (dx, dw, dbias); dx is apart from x and dy, dbias None without a bias."),
     FAST(token_conv_step, "token_conv_step(x, w, bias, state, silu=True, y=None, state_out=None)\n--\n\n"
                           "ptq4vm_token_conv_step: y [B, K] for one token of each sequence; state ([B, W - 1, K]) advances in place unless state_out is given."),
     FAST(residual_norm, "residual_norm(h, residual, w, gate=None, w_post=None, scale=1.0, eps=1e-5, y=None, residual_out=None)\n--\n\n"
-                        "ptq4vm_residual_norm: (y, residual_out); residual_out has residual's type, h's where residual is None and none is given."),
+                        "ptq4vm_residual_norm: (y, residual_out); residual_out has residual's type, h's where residual is None and none is given.\n"
+                        "Records nothing for autograd: gradients come from residual_norm_backward."),
     FAST(residual_norm_backward, "residual_norm_backward(dy, dr, h, r, w, gate=None, w_post=None, scale=1.0, eps=1e-5, first=False, dh=None, dresidual=None)\n--\n\n"
                                  "ptq4vm_residual_norm_backward, r the forward pass's residual_out and dr its gradient or None: (dh, dresidual, dw, dgate,\n"
                                  "dw_post); dresidual is None with first=True (no residual), dgate and dw_post without gate and w_post."),
