@@ -397,7 +397,7 @@ int ptq4vm_gated_scan_step(int dtype, const void *u, const void *dt, const float
  * The backward pass gives dx [B*L, K] T, dw [K, W] f32 and dbias [K] f32 (may be NULL) for the gradient dy of y; the state is a
  * constant.  The step is L = 1 on states that it advances; its state_out may be the buffer of `state`.
  * A token is read again by the runs of tokens beside its own: y may share no element with x, nor dx with x or dy (PTQ4VM_ERR_OVERLAP;
- * halves of one wider matrix share none).  Where L = 1, y may be x itself, and dx x or dy.
+ * halves of one wider matrix share none; with different pitches their ranges may not meet).  Where L = 1, y may be x itself, and dx x or dy.
  * Errors: NULL x / w / y (dy / x / w / dx / dw; x / w / state / y / state_out), sizes out of range (K up to 2^27 - 1, and for y fewer than
  * 2^32 lanes: one for 8 channels of 4 to 16 tokens), ld* < K, misalignment, workspace too small (PTQ4VM_ERR_SHAPE) or missing.
  * B = 0 writes zeros to dw and dbias.
@@ -419,9 +419,9 @@ int ptq4vm_token_conv_step(int dtype, const void *x, const float *w, const float
  *   w [K], w_post [K] f32 in; w_post may be NULL (no norm after the block)
  *   gate     [G, K] f32 in, dense, may be NULL (ones): row i takes gate row i / (M / G), so G = 1 is a gate per channel, G = B one
  *            per image, G = M one per token
- * y is computed from r before it is rounded to stream_dtype.  Sums of squares are fp32: where a row's pass 3.4e38, norm(v) is 0.  The backward pass takes h and r, the gradient dy of y and the
- * gradient dr of r from the blocks behind (may be NULL: zeros) and gives dh [M, K] T, dresidual [M, K] stream_dtype (may be NULL),
- * dw [K], dgate [G, K] and dw_post [K] f32.
+ * y is computed from r before it is rounded to stream_dtype.  Sums of squares are fp32: where a row's pass 3.4e38, norm(v) is 0.
+ * The backward pass takes h and r, the gradient dy of y and the gradient dr of r from the blocks behind (may be NULL: zeros) and gives
+ * dh [M, K] T, dresidual [M, K] stream_dtype (may be NULL), dw [K], dgate [G, K] and dw_post [K] f32.
  * Errors: NULL h / w / y / r (dy / h / r / w / dh / dw, and dgate, dw_post with their inputs), sizes out of range (K up to
  * PTQ4VM_MAX_NORM_K, G that does not divide M), a stream_dtype that is neither, ld* < K, misalignment, workspace too small
  * (PTQ4VM_ERR_SHAPE) or missing.  M = 0 writes zeros to dw, dgate and dw_post.  G of the workspace function is 0 without a gate.

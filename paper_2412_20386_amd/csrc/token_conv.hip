@@ -265,9 +265,8 @@ int check_conv(int dtype, const void *x, const float *w, const float *bias, cons
 // Whether the lanes of one run would write what those of another read: an output's elements among an input's.  A sequence of one token is
 // read by the lanes that write it, so there the two may be the same.
 bool run_overlap(int dtype, const void *out, int64_t ld_out, const void *in, int64_t ld_in, int64_t B, int64_t L, int64_t K) {
-    const int64_t e = (int64_t)dtype_bytes(dtype), rows = B * L;
-    if (L == 1 && out == in && (rows == 1 || ld_out == ld_in)) return false;
-    return overlap(out, ld_out * e, in, ld_in * e, rows, K * e);
+    if (L == 1 && out == in && (B == 1 || ld_out == ld_in)) return false;
+    return overlap(out, ld_out, in, ld_in, B * L, K, (int64_t)dtype_bytes(dtype));
 }
 
 // f(W, WHOLE)

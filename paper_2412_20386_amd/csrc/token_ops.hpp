@@ -38,16 +38,16 @@ inline Tokens<T> tokens(const void *p, int64_t L, int64_t ld, bool reverse) {
     return {reverse ? data + (L - 1) * ld : data, reverse ? -ld : ld, L * ld};
 }
 
-// Whether two matrices of rows x `width` bytes share a byte.  With the same pitch (halves of one matrix, say) this is exact: the second begins q
-// pitches and r bytes behind the first, and its rows meet those q further, and if r + width > pitch those q + 1 further.  With different pitches it is
-// whether their ranges meet.
-inline bool overlap(const void *a, int64_t pitch_a, const void *b, int64_t pitch_b, int64_t rows, int64_t width) {
-    const int64_t from_a = (int64_t)reinterpret_cast<uintptr_t>(a), from_b = (int64_t)reinterpret_cast<uintptr_t>(b), apart = from_b - from_a;
+// Whether two matrices of rows x `width` elements of `size` bytes, which both are aligned to, share one.  With the same pitch (halves of one
+// matrix, say) this is exact: the second begins q pitches and r elements behind the first, and its rows meet those q further, and if r + width >
+// pitch those q + 1 further.  With different pitches it is whether their ranges meet.
+inline bool overlap(const void *a, int64_t pitch_a, const void *b, int64_t pitch_b, int64_t rows, int64_t width, int64_t size) {
+    const int64_t apart = ((int64_t)reinterpret_cast<uintptr_t>(b) - (int64_t)reinterpret_cast<uintptr_t>(a)) / size;
     if (pitch_a != pitch_b) return apart < (__int128)(rows - 1) * pitch_a + width && -apart < (__int128)(rows - 1) * pitch_b + width;
     const int64_t q = apart / pitch_a - (apart % pitch_a < 0), r = apart - q * pitch_a;
-    return (r < width && q > -rows && q < rows) || (r + width > pitch_a && q + 1 > -rows && q + 1 < rows);
+    return (r < width && q > -rows && q < rows) || (width > pitch_a - r && q + 1 > -rows && q + 1 < rows);
 }
-inline bool overlap(const void *a, const void *b, int64_t bytes) { return a && b && overlap(a, bytes, b, bytes, 1, bytes); }
+inline bool overlap(const void *a, const void *b, int64_t bytes) { return a && b && overlap(a, bytes, b, bytes, 1, bytes, 1); }
 
 // Workgroups go to the 8 XCDs in turn, and each XCD has an L2 of its own: work that shares lines or operands gets
 // consecutive numbers, and an XCD a consecutive range of them.  Some numbers are beyond `total`: the caller leaves.

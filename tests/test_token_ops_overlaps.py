@@ -71,3 +71,14 @@ def test_the_status_has_a_text(lib):  # noqa: F811
     from paper_2412_20386_amd import binding
 
     assert "overlap" in binding.status_string(OVERLAP)
+
+
+@pytest.mark.parametrize("name,out,into,ld_out,ld_in", PAIRS)
+def test_pitches_beyond_any_matrix(lib, name, out, into, ld_out, ld_in):  # noqa: F811
+    """Pitches whose bytes pass 64 bits"""
+    at = apart(name)
+    for dtype, pitch in ((0, 1 << 62), (2, 1 << 62), (2, 1 << 61), (0, (1 << 63) - 1)):
+        kw = dict(dtype=dtype, B=1, L=2)
+        assert call(lib, name, **(at | {out: at[into], ld_in: pitch, ld_out: pitch} | kw)) == OVERLAP
+        assert call(lib, name, **(at | {out: at[into], ld_in: pitch, ld_out: K} | kw)) == OVERLAP
+        assert call(lib, name, **(at | {ld_in: pitch, ld_out: pitch} | kw)) == HIP
